@@ -18,6 +18,7 @@
 #include "gift.h"
 #include "gift_ift.h"
 #include "gift_internal.hpp"
+#include "gift_kv_internal.hpp"
 
 using namespace gift;
 
@@ -1487,3 +1488,28 @@ gift_status gift_token_decrypt(const gift_segment_table* st, const uint8_t* bloc
 }
 
 }  // extern "C"
+
+// What the host side of gift_kv.h (gift_kv_host.cpp) shares with this file.
+namespace gift {
+
+void clear_error() noexcept { g_last_error.clear(); }
+
+gift_status report(gift_status s, const char* message) noexcept {
+  try {
+    return fail(s, "%s", message);
+  } catch (...) {  // no memory for the message
+    return s;
+  }
+}
+
+gift_status report_hip(hipError_t e, const char* what) noexcept {
+  try {
+    return hip_fail(e, what);
+  } catch (...) {
+    return GIFT_E_HIP;
+  }
+}
+
+gift_status paged_geometry(const gift_paged_kv* kv) { return check_paged_geometry(kv); }
+
+}  // namespace gift

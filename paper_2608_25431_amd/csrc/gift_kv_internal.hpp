@@ -1,0 +1,49 @@
+// Types shared by the host side (gift_kv_host.cpp) and the kernels
+// (gift_kv.hip) of include/gift_kv.h.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gift_kv.h"
+
+namespace gift {
+
+// Error reporting and the geometry rules of gift_host.cpp.
+void clear_error() noexcept;
+gift_status report(gift_status s, const char* message) noexcept;
+gift_status report_hip(hipError_t e, const char* what) noexcept;
+gift_status paged_geometry(const gift_paged_kv* kv);
+
+// Where K and V of a layer's (block, token, head) lie.
+struct KvView {
+  uint8_t* base;  // of K of block 0, token 0, head 0 (append: of layer 0)
+  int64_t v_off;  // from K to V
+  uint64_t layer_stride, block_stride, token_stride, head_stride;
+  uint64_t n_blocks;
+  uint32_t n_layers, heads, head_dim, block_shift;
+};
+
+struct TablesArgs {
+  gift_kv_step s;
+  uint32_t block_shift;
+};
+hipError_t launch_kv_tables(const TablesArgs& a, hipStream_t s);
+
+struct AppendArgs {
+  KvView kv;
+  gift_kv_rows src;
+  const int64_t* slots;
+  const uint32_t* index;
+  uint32_t n_slots;
+};
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
+
+struct AttnArgs {
+  KvView kv;
+  gift_tree_attention_args a;
+  uint32_t group;  // query heads of a KV head
+};
+hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, hipStream_t s);
+
+}  // namespace gift

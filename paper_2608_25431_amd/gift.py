@@ -1,4 +1,5 @@
-"""ctypes binding of libgift.so (include/gift.h): argument marshalling only.
+"""ctypes binding of libgift.so (include/gift.h, gift_kv.h, gift_ift.h):
+argument marshalling only.
 
 Every entry point has the C name without the ``gift_`` prefix.  Device
 buffers may be passed as torch tensors (their ``data_ptr()`` is used) or as
@@ -19,7 +20,8 @@ LIB_PATH = os.path.join(HERE, "libgift.so")
 
 OK, E_INVALID, E_RANGE, E_OVERLAP, E_NONCE_REUSE, E_TOO_LARGE, E_HIP, E_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7
 E_REJECTED, E_RACE = -8, -9
-SEG_OK, SEG_AUTH_FAIL, SEG_OWNER_MIXED = 0, 1, 2
+SEG_OK, SEG_AUTH_FAIL, SEG_OWNER_MIXED, SEG_NO_SPACE = 0, 1, 2, 3
+BF16, F16 = 1, 2
 LABEL_PARAM, LABEL_UNOWNED = 0xFFFFFFFE, 0xFFFFFFFF
 
 # Host layout of gift_segment (32 bytes).
@@ -62,12 +64,45 @@ class _Request(ctypes.Structure):
                 ("iv_seq", ctypes.c_uint64)]
 
 
+class _KvFormat(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_uint32), ("n_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32),
+                ("block_tokens", ctypes.c_uint32), ("k_offset", ctypes.c_uint64), ("v_offset", ctypes.c_uint64),
+                ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class _KvStep(ctypes.Structure):
+    _fields_ = [("n_reqs", ctypes.c_uint32), ("block_tokens", ctypes.c_uint32), ("n_blocks", ctypes.c_uint64),
+                ("users", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+                ("free_blocks", ctypes.c_void_p), ("n_free", ctypes.c_uint32), ("table_width", ctypes.c_uint32),
+                ("table_stride", ctypes.c_uint64), ("tables", ctypes.c_void_p), ("block_labels", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("n_slots", ctypes.c_uint64), ("row_begin", ctypes.c_void_p),
+                ("lens_out", ctypes.c_void_p), ("taken", ctypes.c_void_p), ("verdicts", ctypes.c_void_p)]
+
+
+class _KvRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_rows", ctypes.c_uint64)] + \
+        [(f"{x}_{d}_stride", ctypes.c_uint64) for x in "kv" for d in ("layer", "row", "head")]
+
+
+class _TreeAttention(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_uint64), ("n_reqs", ctypes.c_uint32), ("n_heads", ctypes.c_uint32),
+                ("layer", ctypes.c_uint32), ("scale", ctypes.c_float), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p)] + \
+        [(f"{x}_{d}_stride", ctypes.c_uint64) for x in ("q", "k", "v", "out") for d in ("row", "head")] + \
+        [("row_begin", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("tables", ctypes.c_void_p),
+         ("table_width", ctypes.c_uint32), ("table_stride", ctypes.c_uint64), ("mask", ctypes.c_void_p),
+         ("mask_words", ctypes.c_uint32), ("verdicts", ctypes.c_void_p)]
+
+
 assert ctypes.sizeof(_Segment) == SEGMENT_DTYPE.itemsize == 32
 
 EXPORTS = ("gift_key_table_create", "gift_key_table_users", "gift_key_table_destroy", "gift_seal", "gift_seal_noalloc",
            "gift_open",
            "gift_check_owner", "gift_seal_paged", "gift_open_paged", "gift_token_encrypt", "gift_token_decrypt", "gift_profile_next_call",
            "gift_status_string", "gift_last_error",
+           # include/gift_kv.h
+           "gift_kv_tables", "gift_kv_append", "gift_attention_work_create", "gift_attention_work_destroy",
+           "gift_tree_attention",
            # include/gift_ift.h
            "gift_own_create", "gift_own_destroy", "gift_own_register", "gift_own_release", "gift_own_units",
            "gift_own_flat_index", "gift_own_set", "gift_own_get", "gift_own_labels", "gift_own_ops",
@@ -109,6 +144,18 @@ def lib():
         L.gift_token_encrypt.restype = st
         L.gift_token_decrypt.argtypes = [ctypes.POINTER(_SegTable), P, ctypes.c_uint64, P, ctypes.c_uint64, P, P, P]
         L.gift_token_decrypt.restype = st
+        L.gift_kv_tables.argtypes = [ctypes.POINTER(_KvStep), P]
+        L.gift_kv_tables.restype = st
+        L.gift_kv_append.argtypes = [ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat), P, ctypes.c_uint64, P,
+                                     ctypes.POINTER(_KvRows), P]
+        L.gift_kv_append.restype = st
+        L.gift_attention_work_create.argtypes = [P, ctypes.POINTER(ctypes.c_void_p)]
+        L.gift_attention_work_create.restype = st
+        L.gift_attention_work_destroy.argtypes = [P]
+        L.gift_attention_work_destroy.restype = st
+        L.gift_tree_attention.argtypes = [P, ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat),
+                                          ctypes.POINTER(_TreeAttention), P]
+        L.gift_tree_attention.restype = st
         L.gift_profile_next_call.argtypes = [P, P]
         L.gift_profile_next_call.restype = st
         L.gift_status_string.argtypes = [st]
@@ -367,6 +414,127 @@ def token_decrypt(segs, blocks, n_tokens, kt, eos_token, tokens_out, nonces_out=
                                     eos_token, _dev(tokens_out, 8 * n_tokens, "tokens_out"),
                                     _dev(nonces_out, 8 * n_tokens, "nonces_out"), _stream(stream)))
     del keep
+
+
+# --- include/gift_kv.h: the paged cache in use on the device ---
+
+def kv_format(dtype, n_heads, head_dim, block_tokens, token_stride, head_stride, v_offset, k_offset=0):
+    """gift_kv_format.  dtype: torch.bfloat16, torch.float16 or their codes (BF16, F16); offsets and strides in bytes."""
+    code = dtype if isinstance(dtype, int) else {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(dtype))
+    if code is None:
+        raise ValueError(f"dtype {dtype}: K and V are bfloat16 or float16")
+    return _KvFormat(code, n_heads, head_dim, block_tokens, k_offset, v_offset, token_stride, head_stride)
+
+
+def _ints(x, n, name, size=4):
+    """Address of a device array of n integers of size bytes (a contiguous tensor of that width, or an address)."""
+    if x is not None and hasattr(x, "element_size") and x.element_size() != size:
+        raise ValueError(f"{name}: elements of {x.element_size()} bytes, the call needs {size}")
+    return _dev(x, size * n, name)
+
+
+def _matrix(x, rows, name):
+    """Address, columns and row stride (in entries) of a device [rows][columns] int32 tensor, rows any distance apart."""
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if x.element_size() != 4 or x.dim() != 2 or x.shape[0] < rows or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: needs {rows} rows of adjacent 32-bit entries")
+    return x.data_ptr(), x.shape[1], max(x.stride(0), x.shape[1]) if x.shape[0] < 2 else x.stride(0)
+
+
+def _rows_of(x, fmt, lead, heads, name):
+    """Address and byte strides of a device tensor [*lead][heads][head_dim] of the format's type, whose last dimension
+    is contiguous; dimensions of one element have stride 0."""
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(x.dtype)) != fmt.dtype:
+        raise ValueError(f"{name}: {x.dtype} is not the cache's type")
+    want = (*lead, heads, fmt.head_dim)
+    if tuple(x.shape) != want:
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {want}")
+    if x.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return x.data_ptr(), [0 if x.shape[d] <= 1 else 2 * x.stride(d) for d in range(len(want) - 1)]
+
+
+def _same_format(kv, fmt):
+    if not isinstance(kv, _PagedKV) or not isinstance(fmt, _KvFormat):
+        raise TypeError("kv and fmt come from paged_kv() and kv_format()")
+
+
+def kv_tables(users, lens, new_lens, block_tokens, free_blocks, tables, block_labels, slots, row_begin, lens_out, taken,
+              verdicts, stream=None):
+    """gift_kv_tables.  Device tensors: users, lens, new_lens, lens_out, verdicts int32 [n_reqs]; free_blocks int32;
+    tables int32 [n_reqs][width]; block_labels int32 [n_blocks]; slots int64 [n_slots]; row_begin int32 [n_reqs + 1];
+    taken int32 [1]."""
+    n = users.numel()
+    tab, width, stride = _matrix(tables, n, "tables")
+    s = _KvStep(n, block_tokens, block_labels.numel(), _ints(users, n, "users"), _ints(lens, n, "lens"),
+                _ints(new_lens, n, "new_lens"), _ints(free_blocks, 0, "free_blocks"), free_blocks.numel(), width, stride,
+                tab, _ints(block_labels, 1, "block_labels"), _ints(slots, 0, "slots", 8), slots.numel(),
+                _ints(row_begin, n + 1, "row_begin"), _ints(lens_out, n, "lens_out"), _ints(taken, 1, "taken"),
+                _ints(verdicts, n, "verdicts"))
+    _check(lib().gift_kv_tables(ctypes.byref(s), _stream(stream)))
+
+
+def kv_append(kv, fmt, slots, k, v, index=None, stream=None):
+    """gift_kv_append.  kv from paged_kv(), fmt from kv_format(); slots device int64 [n_slots]; k, v device tensors
+    [n_layers][n_rows][heads][head_dim], any strides but the last; index device int32 [n_slots] or None."""
+    _same_format(kv, fmt)
+    n = slots.numel()
+    rows = k.shape[1] if k.dim() == 4 else 0
+    kp, ks = _rows_of(k, fmt, (kv.n_layers, rows), fmt.n_heads, "k")
+    vp, vs = _rows_of(v, fmt, (kv.n_layers, rows), fmt.n_heads, "v")
+    r = _KvRows(kp, vp, rows, *ks, *vs)
+    if index is None and rows < n:
+        raise ValueError(f"k: {rows} rows, the call needs {n}")
+    _check(lib().gift_kv_append(ctypes.byref(kv), ctypes.byref(fmt), _ints(slots, n, "slots", 8), n,
+                                _ints(index, n, "index"), ctypes.byref(r), _stream(stream)))
+
+
+class AttentionWork:
+    """Owns a gift_attention_work handle: one for each stream that calls tree_attention."""
+
+    def __init__(self, stream=None):
+        h = ctypes.c_void_p()
+        _check(lib().gift_attention_work_create(_stream(stream), ctypes.byref(h)))
+        self.handle = h.value
+
+    def destroy(self):
+        if self.handle:
+            h, self.handle = self.handle, None
+            _check(lib().gift_attention_work_destroy(h))
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, mask=None, verdicts=None, lse=None,
+                   scale=None, stream=None):
+    """gift_tree_attention.  q, out device tensors [n_rows][n_heads][head_dim]; k, v [n_rows][kv heads][head_dim], or
+    both None; any strides but the last.  row_begin int32 [n_reqs + 1]; lens, verdicts int32 [n_reqs]; tables int32
+    [n_reqs][width]; mask int32 [n_rows][words]; lse float32 [n_rows][n_heads].  scale defaults to head_dim ** -0.5."""
+    _same_format(kv, fmt)
+    n, (rows, heads) = lens.numel(), (q.shape[0], q.shape[1] if q.dim() == 3 else 0)
+    qp, qs = _rows_of(q, fmt, (rows,), heads, "q")
+    op, os_ = _rows_of(out, fmt, (rows,), heads, "out")
+    (kp, ks), (vp, vs) = (_rows_of(x, fmt, (rows,), fmt.n_heads, name) if x is not None else (None, [0, 0])
+                          for x, name in ((k, "k"), (v, "v")))
+    tab, width, stride = _matrix(tables, n, "tables")
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] < rows:
+            raise ValueError(f"mask: needs {rows} rows of words")
+        words = mask.shape[1]
+    a = _TreeAttention(rows, n, heads, layer, fmt.head_dim ** -0.5 if scale is None else scale, qp, kp, vp, op,
+                       _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_, _ints(row_begin, n + 1, "row_begin"),
+                       _ints(lens, n, "lens"), tab, width, stride, _ints(mask, rows * words, "mask"), words,
+                       _ints(verdicts, n, "verdicts"))
+    _check(lib().gift_tree_attention(work.handle, ctypes.byref(kv), ctypes.byref(fmt), ctypes.byref(a),
+                                     _stream(stream)))
 
 
 def profile_next_call(before, after):

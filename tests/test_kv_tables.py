@@ -1,0 +1,131 @@
+"""gift_kv_tables on the GPU against its definition, request by request: lengths around block ends, requests that add
+nothing, short pools and tables, foreign blocks, ids outside the cache, short slot arrays."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+from kv_helpers import DEV, NO_BLOCK, expect_tables, i32  # noqa: E402
+from paper_2608_25431_amd import gift  # noqa: E402
+
+
+def make(r, n, block, lo, hi, nlo, nhi, users, extra_width=1, spare=0):
+    lens, new = r.integers(lo, hi + 1, n), r.integers(nlo, nhi + 1, n)
+    have, want = -(-lens // block), -(-(lens + new) // block)
+    width = max(1, int(want.max()) + extra_width)
+    n_blocks = int(want.sum()) + 8
+    ids = r.permutation(n_blocks)
+    tab = np.full((n, width), NO_BLOCK, np.int64)
+    cached = np.arange(width)[None, :] < have[:, None]
+    tab[cached] = ids[:cached.sum()]
+    free = ids[cached.sum():cached.sum() + max(0, int((want - have).sum()) + spare)]
+    who = r.integers(0, users, n)
+    labels = np.full(n_blocks, gift.LABEL_UNOWNED, np.int64)
+    labels[tab[cached]] = np.broadcast_to(who[:, None], tab.shape)[cached]
+    return dict(users=who, lens=lens, new=new, block=block, free=free, tab=tab, labels=labels, n_slots=int(new.sum()))
+
+
+def run(c, pad=0):
+    n, width = c["tab"].shape
+    store = torch.full((n, width + pad), -5, dtype=torch.int32, device=DEV)  # rows further apart than they are wide
+    tables = store[:, :width]
+    tables.copy_(i32(c["tab"]))
+    out = dict(labels=i32(c["labels"]), slots=torch.full((c["n_slots"],), -77, dtype=torch.int64, device=DEV),
+               row_begin=torch.full((n + 1,), -77, dtype=torch.int32, device=DEV),
+               lens_out=torch.full((n,), -77, dtype=torch.int32, device=DEV),
+               taken=torch.full((1,), -77, dtype=torch.int32, device=DEV),
+               verdicts=torch.full((n,), -77, dtype=torch.int32, device=DEV))
+    gift.kv_tables(i32(c["users"]), i32(c["lens"]), i32(c["new"]), c["block"], i32(c["free"]), tables, out["labels"],
+                   out["slots"], out["row_begin"], out["lens_out"], out["taken"], out["verdicts"])
+    torch.cuda.synchronize()
+    assert (store[:, width:] == -5).all()
+    got = {k: v.cpu().numpy() for k, v in out.items()}
+    got["tables"] = tables.cpu().numpy()
+    return got
+
+
+def check(c, pad=0):
+    got = run(c, pad)
+    want = expect_tables(c["users"], c["lens"], c["new"], c["block"], c["free"], c["tab"], c["labels"], c["n_slots"])
+    for k in want:
+        w = want[k] if k == "slots" else want[k].astype(np.uint32).view(np.int32)
+        assert got[k].shape == w.shape and (got[k] == w).all(), \
+            f"{k}: {(got[k] != w).sum()} differ, first at {np.argwhere(got[k] != w)[:1].tolist()}"
+    return want
+
+
+@pytest.mark.parametrize("n,block,lo,hi,nlo,nhi", [
+    (1, 16, 0, 0, 1, 1), (1, 1, 5, 5, 3, 3), (3, 16, 15, 17, 0, 2), (5, 2, 0, 9, 0, 9), (64, 16, 128, 2048, 1, 4),
+    (300, 16, 0, 100, 0, 40), (257, 8, 0, 64, 0, 17), (1025, 16, 0, 40, 0, 4),       # one wave for a request
+    (7, 16, 0, 0, 3000, 6000), (20, 1, 0, 300, 0, 300),                              # a workgroup of 256
+    (2, 16, 0, 0, 9000, 40000), (3, 8, 60000, 70000, 1, 33), (5, 1, 0, 5000, 0, 0)])  # of 1024
+def test_lengths(n, block, lo, hi, nlo, nhi):
+    r = np.random.default_rng(n + block)
+    want = check(make(r, n, block, lo, hi, nlo, nhi, max(1, n // 2)), pad=n % 3)
+    assert (want["verdicts"] == gift.SEG_OK).all()
+
+
+@pytest.mark.parametrize("spare", [-1, -5, -10000, 3])
+@pytest.mark.parametrize("n,hi,nhi", [(40, 70, 40), (600, 20, 20), (9, 30, 9000)])
+def test_short_pools(n, hi, nhi, spare):
+    r = np.random.default_rng(n)
+    want = check(make(r, n, 16, 0, hi, 0, nhi, 3, spare=spare))
+    if spare < 0:
+        assert (want["verdicts"] == gift.SEG_NO_SPACE).any()
+
+
+def test_short_tables_take_nothing():
+    r = np.random.default_rng(5)
+    c = make(r, 50, 16, 0, 100, 0, 60, 4)
+    width = c["tab"].shape[1] - 3
+    c["tab"] = np.ascontiguousarray(c["tab"][:, :width])  # some requests' new tokens, or cached ones, do not fit
+    want = check(c)
+    assert (want["verdicts"] == gift.SEG_NO_SPACE).any() and (want["verdicts"] == gift.SEG_OK).any()
+
+
+def test_lengths_past_32_bits_of_sum():
+    c = make(np.random.default_rng(6), 4, 16, 0, 30, 0, 9, 2)
+    c["lens"][2], c["new"][2] = 0xFFFFFFF0, 0xFFFFFFFF  # no table row holds that, and their sum has 33 bits
+    c["n_slots"] = 64
+    want = check(c)
+    assert want["verdicts"][2] != gift.SEG_OK and want["verdicts"][1] == gift.SEG_OK
+
+
+@pytest.mark.parametrize("n,hi,nhi", [(30, 200, 20), (6, 30000, 3)])
+def test_foreign_blocks(n, hi, nhi):
+    r = np.random.default_rng(n)
+    c = make(r, n, 16, 40, hi, 0, nhi, 3)
+    have = -(-c["lens"] // 16)
+    c["labels"][c["tab"][1, have[1] - 1]] = c["users"][1] + 1                       # last block of another user
+    c["labels"][c["tab"][2, 0]] = gift.LABEL_PARAM
+    c["tab"][3, have[3] // 2] = len(c["labels"])                                     # first id outside the cache
+    c["tab"][4, 0] = 0xFFFFFFFF
+    want = check(c)
+    assert (want["verdicts"][1:5] == gift.SEG_OWNER_MIXED).all() and want["verdicts"][0] == gift.SEG_OK
+
+
+def test_free_ids_outside_the_cache():
+    c = make(np.random.default_rng(8), 20, 16, 0, 50, 17, 60, 3)
+    c["free"][7] = len(c["labels"])
+    c["free"][20] = 0xFFFFFFFF
+    want = check(c)
+    assert (want["verdicts"] == gift.SEG_NO_SPACE).sum() == 2
+
+
+@pytest.mark.parametrize("delta", [-9, 9])
+def test_slot_arrays_of_other_lengths(delta):
+    c = make(np.random.default_rng(9), 33, 16, 0, 50, 0, 12, 3)
+    c["n_slots"] += delta
+    want = check(c)
+    assert (want["verdicts"] == gift.SEG_OK).all() == (delta > 0)
+
+
+def test_no_requests():
+    slots = torch.full((5,), 3, dtype=torch.int64, device=DEV)
+    empty = torch.zeros(0, dtype=torch.int32, device=DEV)
+    first, taken = torch.full((1,), 9, dtype=torch.int32, device=DEV), torch.full((1,), 9, dtype=torch.int32, device=DEV)
+    gift.kv_tables(empty, empty, empty, 16, empty, torch.zeros(0, 4, dtype=torch.int32, device=DEV), i32([0, 1]), slots,
+                   first, empty, taken, empty)
+    assert slots.tolist() == [-1] * 5 and first.item() == 0 and taken.item() == 0
