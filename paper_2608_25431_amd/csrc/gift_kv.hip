@@ -216,104 +216,527 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // Attention
 // ---------------------------------------------------------------------------
 
+// The rows of a request that read one KV head (its tokens times the query
+// heads of the head) form the columns of 32-wide tiles, keys the rows:
+//     S^T = K Q^T,   P = exp2(c (S - max)),   O^T += V^T P^T
+// on the 32x32x16 matrix instruction.  With keys as rows, a lane holds scores
+// of one query only, so the maximum and the sum of a softmax row stay in the
+// lane (and its partner 32 lanes on), rescaling O is one factor per lane, and
+// the registers that hold P^T are the second product's operand as they are:
+// the order of keys in a contraction is free, so V^T is read in the same
+// order, four keys at a time, by the transposing LDS read.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
 struct Bf16 {
-  __device__ static float up(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-  __device__ static uint16_t down(float f) {
-    const __bf16 b = (__bf16)f;
-    return __builtin_bit_cast(uint16_t, b);
+  typedef bf16x8 vec;
+  typedef __bf16 elem;
+  static constexpr uint32_t kExp = 0x7F80;  // exponent bits: all set in NaN and infinities
+  // Weights are 8 bits of bfloat16 in two operands, the upper half of the float and what is left of it: with one
+  // operand their rounding would add as much error again as the output's own.
+  static constexpr int kParts = 2;
+  __device__ static void parts(const f32x16& p, int k, vec* w) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const uint32_t x = __float_as_uint(p[8 * k + i]);
+      w[0][i] = __builtin_bit_cast(elem, (uint16_t)(x >> 16));
+      w[1][i] = (elem)(p[8 * k + i] - __uint_as_float(x & 0xFFFF0000u));
+    }
   }
+  __device__ static f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
-  __device__ static float up(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
-  __device__ static uint16_t down(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
+  typedef f16x8 vec;
+  typedef _Float16 elem;
+  static constexpr uint32_t kExp = 0x7C00;
+  // one operand: 11 bits of weights against 11 of the output
+  static constexpr int kParts = 1;
+  __device__ static void parts(const f32x16& p, int k, vec* w) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) w[0][i] = (elem)p[8 * k + i];
+  }
+  __device__ static f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-template <class E>
-__device__ float dot8(uint4 x, uint4 y) {
-  const uint32_t* p = (const uint32_t*)&x;
-  const uint32_t* q = (const uint32_t*)&y;
-  float s = 0;
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    s += E::up((uint16_t)p[i]) * E::up((uint16_t)q[i]);
-    s += E::up((uint16_t)(p[i] >> 16)) * E::up((uint16_t)(q[i] >> 16));
-  }
-  return s;
+constexpr int kTileKeys = 32;
+
+// WQ waves share a tile of keys, each with 32 columns of its own; WK groups of
+// them take different keys, TK tiles a group in a round.
+template <int D_, int WQ_, int WK_, int TK_>
+struct Shape {
+  static constexpr int D = D_, WQ = WQ_, WK = WK_, TK = TK_;
+  static constexpr int kWaves = WQ * WK, kThreads = kWave * kWaves, kTiles = WK * TK;  // per round
+  // a wave that shares its tiles with no other needs no second buffer: its LDS accesses are in order
+  static constexpr int kBufs = WQ == 1 ? 1 : 2;
+  // LDS rows are padded so that the 16-byte reads of K down a column and the transposing reads of V over four rows
+  // fall into different banks
+  static constexpr int kKRow = 2 * D + 16, kVRow = 2 * D + 32, kTileBytes = kTileKeys * (kKRow + kVRow);
+  // a row's 16-byte pieces go to a power of two of lanes (D = 96: 12 of 16 lanes load)
+  static constexpr int kPieces = D / 8, kLanes = D <= 64 ? 8 : D <= 128 ? 16 : 32, kRowsAtOnce = kWave / kLanes;
+  static constexpr int kLoads = kTileKeys * TK / (kRowsAtOnce * WQ);  // 16-byte loads of K (and of V) per lane and round
+  static constexpr int kRows = kRowsAtOnce * kLoads;                  // rows that a wave loads in a round
+  static constexpr int kAcc = D / 32;
+  static constexpr int kTileArea = kBufs * kTiles * kTileBytes, kMergeArea = (kWaves - WQ) * (kAcc * 4096 + 512);
+  static constexpr int kArea = kTileArea > kMergeArea ? kTileArea : kMergeArea;
+  static constexpr size_t kPartial = (size_t)WQ * (kAcc * 4096 + 512);
+  static_assert(kLoads >= 1 && kRows <= kWave, "rows of a round");
+};
+
+// A request as the kernel works on it.
+struct Req {
+  uint32_t row0, rows, len, ctx_tiles, tiles, rounds, cols, col_tiles;
+  bool dead;  // rejected: zeros
+};
+
+template <class S>
+__device__ Req req_of(const AttnArgs& p, uint32_t b) {
+  const gift_tree_attention_args& a = p.a;
+  Req r;
+  const uint32_t total = (uint32_t)a.n_rows;
+  uint32_t lo = a.row_begin[b], hi = a.row_begin[b + 1];
+  lo = lo < total ? lo : total;
+  hi = hi < total ? hi : total;
+  r.row0 = lo;
+  r.rows = hi > lo ? hi - lo : 0;
+  const uint32_t most = a.table_width << p.kv.block_shift, len = a.lens[b];
+  r.len = len < most ? len : most;
+  r.dead = a.verdicts && a.verdicts[b] != GIFT_SEG_OK;
+  r.ctx_tiles = (r.len + kTileKeys - 1) / kTileKeys;
+  r.tiles = r.ctx_tiles + (a.k ? (r.rows + kTileKeys - 1) / kTileKeys : 0);
+  const uint32_t rounds = (r.tiles + S::kTiles - 1) / S::kTiles;
+  r.rounds = r.dead || rounds == 0 ? 1 : rounds;
+  r.col_tiles = (uint32_t)(((uint64_t)r.rows * p.group + 32 * S::WQ - 1) / (32 * S::WQ));
+  r.cols = r.col_tiles * p.kv.heads;
+  return r;
 }
 
-// One wave per (row, query head).  A lane scores one key of 64 at a time, then
-// the wave adds the keys' V rows, each lane head_dim / 64 elements.
-template <class E>
-__global__ __launch_bounds__(256) void k_attention_plain(AttnArgs p) {
-  const gift_tree_attention_args& a = p.a;
-  const uint64_t unit = (uint64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-  const uint32_t lane = threadIdx.x % kWave;
-  if (unit >= a.n_rows * a.n_heads) return;
-  const uint32_t r = (uint32_t)(unit / a.n_heads), h = (uint32_t)(unit % a.n_heads), g = h / p.group;
-  const uint32_t D = p.kv.head_dim;
-  uint32_t b = a.n_reqs, r0 = 0, r1 = 0;
-  for (uint32_t i = 0; i < a.n_reqs; i++)
-    if (r >= a.row_begin[i] && r < a.row_begin[i + 1]) {
-      b = i;
-      break;
-    }
-  float m = -INFINITY, l = 0, acc[4] = {0, 0, 0, 0};
-  if (b < a.n_reqs && (!a.verdicts || a.verdicts[b] == GIFT_SEG_OK)) {
-    r0 = a.row_begin[b];
-    r1 = a.row_begin[b + 1] < a.n_rows ? a.row_begin[b + 1] : (uint32_t)a.n_rows;
-    const uint32_t most = a.table_width << p.kv.block_shift, len = a.lens[b] < most ? a.lens[b] : most;
-    const uint32_t n = a.k ? r1 - r0 : 0;
-    const uint8_t* q = (const uint8_t*)a.q + r * a.q_row_stride + h * a.q_head_stride;
-    for (uint32_t j0 = 0; j0 < len + n; j0 += kWave) {
-      const uint32_t j = j0 + lane;
-      const uint8_t *kp = nullptr, *vp = nullptr;
-      if (j < len) {
-        const uint32_t id = a.tables[b * a.table_stride + (j >> p.kv.block_shift)];
-        if (id < p.kv.n_blocks) {
-          kp = p.kv.base + a.layer * p.kv.layer_stride + id * p.kv.block_stride +
-               (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride + g * p.kv.head_stride;
-          vp = kp + p.kv.v_off;
-        }
-      } else if (j < len + n) {
-        const uint32_t t = j - len;
-        const bool see = a.mask ? t < 32ull * a.mask_words && ((a.mask[(uint64_t)r * a.mask_words + t / 32] >> (t % 32)) & 1)
-                                : t <= r - r0;
-        if (see) {
-          kp = (const uint8_t*)a.k + (r0 + t) * a.k_row_stride + g * a.k_head_stride;
-          vp = (const uint8_t*)a.v + (r0 + t) * a.v_row_stride + g * a.v_head_stride;
-        }
-      }
-      float s = -INFINITY;
-      if (kp) {
-        s = 0;
-        for (uint32_t c = 0; c < D / 8; c++) s += dot8<E>(*(const uint4*)(q + 16 * c), *(const uint4*)(kp + 16 * c));
-        s *= a.scale;
-      }
-      float top = s;
-      for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-      const float m2 = fmaxf(m, top), safe = m2 == -INFINITY ? 0.f : m2, fix = expf(m - safe);
-      const float w = kp ? expf(s - safe) : 0.f;
-      float sum = w;
-      for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
-      l = l * fix + sum;
-      m = m2;
-      for (int i = 0; i < 4; i++) acc[i] *= fix;
-      for (int j2 = 0; j2 < kWave; j2++) {
-        const uint8_t* row = (const uint8_t*)__shfl((unsigned long long)vp, j2);
-        if (!row) continue;
-        const float wj = __shfl(w, j2);
+// Running state of one wave's 32 columns: lane l holds column l % 32; of O^T
+// the elements d = 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
+template <class S>
+struct State {
+  float m, l;  // maximum (unscaled score), this lane's part of the sum
+  f32x16 o[S::kAcc];
+  __device__ void clear() {
+    m = -INFINITY;
+    l = 0;
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-          if (lane + 64 * i < D) acc[i] += wj * E::up(*(const uint16_t*)(row + 2 * (lane + 64 * i)));
+    for (int t = 0; t < S::kAcc; t++) o[t] = f32x16{};
+  }
+  // Adds a state with the whole sum l2 (given to one of the two lanes of a column).
+  __device__ void add(float m2, float l2, const float4* src, float c) {
+    const float mn = fmaxf(m, m2), safe = mn == -INFINITY ? 0.f : mn;
+    const float f1 = exp2f((m - safe) * c), f2 = exp2f((m2 - safe) * c);
+    m = mn;
+    l = l * f1 + l2 * f2;
+#pragma unroll
+    for (int t = 0; t < S::kAcc; t++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const float4 v = src[(t * 4 + q) * kWave];
+        o[t][4 * q] = o[t][4 * q] * f1 + v.x * f2;
+        o[t][4 * q + 1] = o[t][4 * q + 1] * f1 + v.y * f2;
+        o[t][4 * q + 2] = o[t][4 * q + 2] * f1 + v.z * f2;
+        o[t][4 * q + 3] = o[t][4 * q + 3] * f1 + v.w * f2;
       }
+  }
+  // dst: [kAcc * 4][64] float4, then [64] (m, l)
+  __device__ void put(float4* dst, uint32_t lane) const {
+#pragma unroll
+    for (int t = 0; t < S::kAcc; t++)
+#pragma unroll
+      for (int q = 0; q < 4; q++)
+        dst[(t * 4 + q) * kWave + lane] = make_float4(o[t][4 * q], o[t][4 * q + 1], o[t][4 * q + 2], o[t][4 * q + 3]);
+    ((float2*)(dst + S::kAcc * 4 * kWave))[lane] = make_float2(m, l);
+  }
+};
+
+__device__ inline uint64_t uniform(uint64_t x) {
+  return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | __builtin_amdgcn_readfirstlane((uint32_t)x);
+}
+
+__device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Work is cut evenly: a round (kTiles tiles of 32 keys) of a column tile (32 WQ
+// rows of one request and KV head) is a unit, and of all units in a row every
+// workgroup takes the same number, whichever requests they belong to.  A column
+// whose units lie in several workgroups is joined by the one that finishes last,
+// in the order of the parts, so that the result does not depend on who that is.
+template <class E, class S, int MINW>
+__global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p, uint8_t* work) {
+  typedef typename E::vec vec;
+  const gift_tree_attention_args& a = p.a;
+  __shared__ __align__(16) uint8_t area[S::kArea];
+  __shared__ uint8_t row_flags[S::kBufs][S::kTiles][kTileKeys];  // bit 0: the key exists, bit 1: its V is not finite
+  __shared__ uint64_t sums[S::kWaves];
+  __shared__ uint64_t found[2];
+  __shared__ uint32_t last_one;
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave),
+                 wq = wave % S::WQ, wk = wave / S::WQ, half = lane / 32, col = lane % 32;
+  uint32_t n_wg = gridDim.x, wg = blockIdx.x;
+
+  // rows of no request
+  {
+    const uint32_t total = (uint32_t)a.n_rows;
+    uint32_t lo = a.n_reqs ? a.row_begin[0] : 0, hi = a.n_reqs ? a.row_begin[a.n_reqs] : 0;
+    lo = lo < total ? lo : total;
+    hi = hi < lo ? lo : hi < total ? hi : total;
+    const uint32_t loose = lo + (total - hi);
+    for (uint32_t i = wg; i < loose; i += n_wg) {
+      const uint32_t r = i < lo ? i : hi + (i - lo);
+      for (uint32_t u = tid; u < a.n_heads * S::kPieces; u += S::kThreads)
+        *(uint4*)((uint8_t*)a.out + r * a.out_row_stride + u / S::kPieces * a.out_head_stride + u % S::kPieces * 16) =
+            make_uint4(0, 0, 0, 0);
+      if (a.lse)
+        for (uint32_t h = tid; h < a.n_heads; h += S::kThreads) a.lse[(uint64_t)r * a.n_heads + h] = -INFINITY;
     }
   }
-  uint8_t* o = (uint8_t*)a.out + r * a.out_row_stride + h * a.out_head_stride;
+  if (a.n_reqs == 0) return;
+
+  // this workgroup's units, and the request that holds the first of them
+  const uint32_t per = (a.n_reqs + S::kThreads - 1) / S::kThreads;
+  uint64_t mine = 0;
+  for (uint32_t i = 0; i < per; i++) {
+    const uint32_t b = tid * per + i;
+    if (b < a.n_reqs) {
+      const Req r = req_of<S>(p, b);
+      mine += (uint64_t)r.cols * r.rounds;
+    }
+  }
+  uint64_t upto = mine;
 #pragma unroll
-  for (int i = 0; i < 4; i++)
-    if (lane + 64 * i < D)
-      *(uint16_t*)(o + 2 * (lane + 64 * i)) = E::down(m == -INFINITY ? 0.f : acc[i] / l);
-  if (a.lse && lane == 0) a.lse[(uint64_t)r * a.n_heads + h] = m == -INFINITY ? -INFINITY : m + logf(l);
+  for (int d = 1; d < kWave; d *= 2) {
+    const uint64_t u = __shfl_up((unsigned long long)upto, d);
+    if (lane >= (uint32_t)d) upto += u;
+  }
+  if (lane == kWave - 1) sums[wave] = upto;
+  __syncthreads();
+  uint64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < S::kWaves; w++) {
+    if ((uint32_t)w < wave) upto += sums[w];
+    total += sums[w];
+  }
+  total = uniform(total);
+  if (total < n_wg) {
+    if (wg >= total) return;
+    n_wg = (uint32_t)total;  // a unit each
+  } else if (n_wg % 8 == 0) {
+    // neighbours in the order of work share an XCD (and its L2), where column tiles of one KV head read the same keys
+    wg = wg % 8 * (n_wg / 8) + wg / 8;
+  }
+  uint64_t unit = wg * total / n_wg;
+  const uint64_t unit_end = (wg + 1ull) * total / n_wg;
+  if (upto - mine <= unit && unit < upto) {
+    uint64_t at = upto - mine;
+    uint32_t b = tid * per;
+    for (;; b++) {
+      const Req r = req_of<S>(p, b);
+      const uint64_t n = (uint64_t)r.cols * r.rounds;
+      if (unit < at + n) break;
+      at += n;
+    }
+    found[0] = b;
+    found[1] = at;
+  }
+  __syncthreads();
+  uint32_t b = __builtin_amdgcn_readfirstlane((uint32_t)found[0]);
+  uint64_t base = uniform(found[1]);  // first unit of request b
+
+  const float c = fmaxf(fabsf(a.scale) * 1.44269504f, 1.17549435e-38f);
+  const uint32_t neg = a.scale < 0 ? 0x80008000u : 0u;
+  const uint32_t row_lane = lane % S::kRows;  // the row whose address this lane works out
+  // of the group's TK * 32 rows
+  const uint32_t my_row = wq * S::kRowsAtOnce + row_lane % S::kRowsAtOnce + row_lane / S::kRowsAtOnce * (S::kRowsAtOnce * S::WQ);
+  const uint32_t piece = lane % S::kLanes, at_once = lane / S::kLanes;
+  uint32_t* counters = (uint32_t*)work;
+  uint8_t* partials = work + 4 * kAttnCounters;
+
+  Req r = req_of<S>(p, b);
+  while (unit < unit_end) {
+    while (unit >= base + (uint64_t)r.cols * r.rounds) {
+      base += (uint64_t)r.cols * r.rounds;
+      r = req_of<S>(p, ++b);
+    }
+    const uint32_t at = (uint32_t)(unit - base), column = at / r.rounds, it0 = at % r.rounds;
+    const uint64_t col_first = unit - it0, col_last = col_first + r.rounds - 1;
+    const uint32_t it1 = (uint32_t)(unit_end - unit < r.rounds - it0 ? it0 + (unit_end - unit) : r.rounds);
+    const uint32_t g = column / r.col_tiles, ct = column % r.col_tiles;
+    // this lane's query row
+    const uint32_t rows = r.rows * p.group, qrow = (ct * S::WQ + wq) * 32 + col;
+    const bool qlive = qrow < rows;
+    const bool wave_live = (ct * S::WQ + wq) * 32 < rows;
+    const uint32_t token = qlive ? qrow / p.group : 0, head = g * p.group + (qlive ? qrow % p.group : 0);
+    const uint64_t qtok = r.row0 + token;
+    State<S> st;
+    st.clear();
+    if (!r.dead && r.tiles) {
+      vec q[S::D / 16];
+      {
+        const uint8_t* qp = (const uint8_t*)a.q + qtok * a.q_row_stride + head * a.q_head_stride + half * 16;
+#pragma unroll
+        for (int s = 0; s < S::D / 16; s++) {
+          uint4 x = *(const uint4*)(qp + 32 * s);
+          x.x ^= neg, x.y ^= neg, x.z ^= neg, x.w ^= neg;
+          q[s] = __builtin_bit_cast(vec, x);
+        }
+      }
+      const uint32_t* tab = a.tables + b * a.table_stride;
+      const uint8_t* kbase = p.kv.base + a.layer * p.kv.layer_stride + g * p.kv.head_stride;
+      const uint8_t *dk = (const uint8_t*)a.k + r.row0 * a.k_row_stride + g * a.k_head_stride,
+                    *dv = (const uint8_t*)a.v + r.row0 * a.v_row_stride + g * a.v_head_stride;
+      const uint32_t ctx_keys = r.ctx_tiles * kTileKeys;
+
+      // first step of a round's loads: the block id of this lane's row
+      auto block_of = [&](uint32_t it) -> uint32_t {
+        const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
+        return j < r.len ? tab[j >> p.kv.block_shift] : 0u;
+      };
+      uint4 kx[S::kLoads], vx[S::kLoads];
+      bool row_ok = false;
+      bool drafted = false;  // the round's rows of this wave may hold drafted keys
+      // second step: addresses of the rows, handed to the lanes that load them
+      auto load = [&](uint32_t it, uint32_t id) {
+        const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
+        const uint8_t *kp, *vp;
+        if (j < ctx_keys) {
+          row_ok = j < r.len && id < p.kv.n_blocks;
+          kp = kbase + id * p.kv.block_stride + (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride;
+          vp = kp + p.kv.v_off;
+        } else {
+          const uint32_t t = j - ctx_keys;
+          row_ok = a.k && t < r.rows;
+          kp = dk + t * a.k_row_stride;
+          vp = dv + t * a.v_row_stride;
+        }
+        if (!row_ok) kp = vp = (const uint8_t*)a.q;  // any row that may be read: nothing of it is used
+        drafted = (it * S::kTiles + wk * S::TK + S::TK) * kTileKeys > ctx_keys;
+#pragma unroll
+        for (int i = 0; i < S::kLoads; i++) {
+          const int from = i * S::kRowsAtOnce + at_once;
+          const uint8_t *kr = (const uint8_t*)__shfl((unsigned long long)kp, from),
+                        *vr = (const uint8_t*)__shfl((unsigned long long)vp, from);
+          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
+            kx[i] = *(const uint4*)(kr + piece * 16);
+            vx[i] = *(const uint4*)(vr + piece * 16);
+          }
+        }
+      };
+      // third step: into LDS.  V rows of keys that do not exist, and drafted ones that are not finite, are stored as
+      // zeros: a weight of zero times NaN would reach every row.
+      auto store = [&](uint32_t buf) {
+        uint32_t flag = row_ok ? 1u : 0u;
+        const uint64_t oks = __ballot(row_ok);
+#pragma unroll
+        for (int i = 0; i < S::kLoads; i++) {
+          const uint32_t slot = i * S::kRowsAtOnce + at_once;
+          bool keep = (oks >> slot) & 1;
+          if (drafted) {
+            const uint32_t w[4] = {vx[i].x, vx[i].y, vx[i].z, vx[i].w};
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              odd |= (w[e] & E::kExp) == E::kExp || (w[e] >> 16 & E::kExp) == E::kExp;
+            const uint64_t odds = __ballot(odd && keep && piece < (uint32_t)S::kPieces);
+            const uint64_t lanes = S::kLanes == 64 ? ~0ull : (1ull << (S::kLanes % 64)) - 1;
+            if (odds >> (at_once * S::kLanes) & lanes) keep = false;
+            if (row_lane / S::kRowsAtOnce == (uint32_t)i && (odds >> (row_lane % S::kRowsAtOnce * S::kLanes) & lanes)) flag |= 2u;
+          }
+          const uint32_t row = wq * S::kRowsAtOnce + at_once + i * (S::kRowsAtOnce * S::WQ);
+          uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + row / kTileKeys) * S::kTileBytes;
+          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
+            *(uint4*)(tile + row % kTileKeys * S::kKRow + piece * 16) = kx[i];
+            *(uint4*)(tile + kTileKeys * S::kKRow + row % kTileKeys * S::kVRow + piece * 16) =
+                keep ? vx[i] : make_uint4(0, 0, 0, 0);
+          }
+        }
+        if (lane < (uint32_t)S::kRows) row_flags[buf][wk * S::TK + my_row / kTileKeys][my_row % kTileKeys] = (uint8_t)flag;
+      };
+      auto meet = [&]() {
+        if constexpr (S::WQ == 1) {
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+        } else {
+          __syncthreads();
+        }
+      };
+      auto compute = [&](uint32_t it, uint32_t buf) {
+#pragma unroll 1
+        for (int s = 0; s < S::TK; s++) {
+          const uint32_t t = it * S::kTiles + wk * S::TK + s;
+          if (t >= r.tiles) break;
+          const uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + s) * S::kTileBytes;
+          const uint32_t flag = row_flags[buf][wk * S::TK + s][col];
+          const bool draft = t >= r.ctx_tiles;
+          uint32_t see = ~0u;
+          if (draft) {
+            const uint32_t w = t - r.ctx_tiles;
+            if (a.mask)
+              see = w < a.mask_words ? a.mask[qtok * a.mask_words + w] : 0u;
+            else
+              see = token >= 32 * w + 31 ? ~0u : token < 32 * w ? 0u : (2u << (token - 32 * w)) - 1;
+          }
+          f32x16 sc = f32x16{};
+          const uint8_t* krow = tile + col * S::kKRow + half * 16;
+#pragma unroll
+          for (int d = 0; d < S::D / 16; d++) sc = E::mfma(*(const vec*)(krow + 32 * d), q[d], sc);
+          const uint32_t have = (uint32_t)__ballot(flag & 1);
+          see &= have;
+          const bool part = draft || have != ~0u;
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+              if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1)) sc[i] = -INFINITY;
+          }
+          float top = sc[0];
+#pragma unroll
+          for (int i = 1; i < 16; i++) top = fmaxf(top, sc[i]);
+          top = fmaxf(top, other_half(top));
+          const float mn = fmaxf(st.m, top), safe = mn == -INFINITY ? 0.f : mn;
+          if (__any(mn != st.m)) {
+            const float f = exp2f((st.m - safe) * c);
+            st.l *= f;
+#pragma unroll
+            for (int d = 0; d < S::kAcc; d++) st.o[d] *= f;
+            st.m = mn;
+          }
+          const float shift = -safe * c;
+#pragma unroll
+          for (int i = 0; i < 16; i++) sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], c, shift));
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+              if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1)) sc[i] = 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; i++) st.l += sc[i];
+          // weights to the operands' type; the sum above is not rounded
+          vec w[2][E::kParts];
+          E::parts(sc, 0, w[0]);
+          E::parts(sc, 1, w[1]);
+          const uint8_t* vrow = tile + kTileKeys * S::kKRow + (4 * half + lane % 16 / 4) * S::kVRow + (lane / 16 % 2 * 16 + lane % 4 * 4) * 2;
+#pragma unroll
+          for (int d = 0; d < S::kAcc; d++)
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+              typedef __attribute__((address_space(3))) s16x4 lds4;
+              union {
+                s16x4 x[2];
+                vec v;
+              } u;
+              u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 16 * k * S::kVRow + 64 * d));
+              u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + (16 * k + 8) * S::kVRow + 64 * d));
+#pragma unroll
+              for (int e = 0; e < E::kParts; e++) st.o[d] = E::mfma(u.v, w[k][e], st.o[d]);
+            }
+          uint32_t odd = draft ? (uint32_t)__ballot(flag & 2) : 0u;
+          if (odd) {  // drafted keys whose V is not finite: only for the rows that see them
+            while (odd) {
+              const uint32_t key = __builtin_ctz(odd);
+              odd &= odd - 1;
+              float mine = 0;
+#pragma unroll
+              for (int i = 0; i < 16; i++)
+                if ((uint32_t)(8 * (i / 4) + i % 4) == (key & ~4u)) mine = sc[i];
+              const float theirs = other_half(mine), weight = (key >> 2 & 1) == half ? mine : theirs;
+              const typename E::elem* vp = (const typename E::elem*)(dv + (uint64_t)((t - r.ctx_tiles) * kTileKeys + key) * a.v_row_stride);
+              if (see >> key & 1) {
+#pragma unroll
+                for (int d = 0; d < S::kAcc; d++)
+#pragma unroll
+                  for (int i = 0; i < 16; i++) st.o[d][i] += weight * (float)vp[32 * d + 8 * (i / 4) + 4 * half + i % 4];
+              }
+            }
+          }
+        }
+      };
+
+      uint32_t id = block_of(it0);
+      load(it0, id);
+      id = it0 + 1 < it1 ? block_of(it0 + 1) : 0u;
+      store(0);
+      meet();
+      for (uint32_t it = it0; it < it1; it++) {
+        const uint32_t buf = S::kBufs == 1 ? 0 : (it - it0) & 1;
+        const bool more = it + 1 < it1;
+        if (more) {
+          load(it + 1, id);
+          id = it + 2 < it1 ? block_of(it + 2) : 0u;
+        }
+        if (wave_live) compute(it, buf);
+        if (more) store(S::kBufs == 1 ? 0 : buf ^ 1);
+        meet();
+      }
+      st.l += other_half(st.l);
+    }
+
+    // the key groups' states meet in the first group
+    auto merge = [&]() {
+      if constexpr (S::WK > 1) {
+        constexpr int kFloat4 = S::kAcc * 4 * kWave + kWave / 2;
+        __syncthreads();
+        if (wk > 0) st.put((float4*)area + (size_t)(wave - S::WQ) * kFloat4, lane);
+        __syncthreads();
+        if (wk == 0) {
+#pragma unroll 1
+          for (int k = 1; k < S::WK; k++) {
+            const float4* src = (const float4*)area + (size_t)((k - 1) * S::WQ + wq) * kFloat4;
+            const float2 ml = ((const float2*)(src + S::kAcc * 4 * kWave))[lane];
+            st.add(ml.x, ml.y, src + lane, c);
+          }
+        }
+      }
+    };
+    merge();
+    auto finish = [&]() {
+      if (wk > 0 || !qlive) return;
+      const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+      uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8;
+#pragma unroll
+      for (int t = 0; t < S::kAcc; t++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          typename E::elem x[4];
+#pragma unroll
+          for (int i = 0; i < 4; i++) x[i] = (typename E::elem)(st.o[t][4 * k + i] * inv);
+          *(uint2*)(op + 64 * t + 16 * k) = __builtin_bit_cast(uint2, x);
+        }
+      if (a.lse && half == 0)
+        a.lse[qtok * a.n_heads + head] = st.l == 0.f ? -INFINITY : (st.m * c + log2f(st.l)) * 0.693147181f;
+    };
+    const uint32_t w0 = (uint32_t)(((col_first + 1) * n_wg - 1) / total), w1 = (uint32_t)(((col_last + 1) * n_wg - 1) / total);
+    if (w0 == w1) {
+      finish();
+    } else {
+      // of a workgroup's parts at most the first joins a column begun before it, and at most the last one begins a
+      // column that others end: two places each
+      const uint32_t place = 2 * wg + (wg == w0 ? 1 : 0);
+      if (wk == 0) st.put((float4*)(partials + place * S::kPartial) + (size_t)wq * (S::kAcc * 4 * kWave + kWave / 2), lane);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const uint32_t parts = w1 - w0 + 1, before = atomicAdd(&counters[w0], 1u);
+        last_one = before == parts - 1;
+        if (before == parts - 1) atomicExch(&counters[w0], 0u);  // clear for the next call
+      }
+      __syncthreads();
+      if (last_one) {
+        __threadfence();
+        st.clear();
+        for (uint32_t w = w0 + wk; w <= w1; w += S::WK) {
+          const float4* src = (const float4*)(partials + (2 * w + (w == w0 ? 1 : 0)) * S::kPartial) +
+                              (size_t)wq * (S::kAcc * 4 * kWave + kWave / 2);
+          const float2 ml = ((const float2*)(src + S::kAcc * 4 * kWave))[lane];
+          st.add(ml.x, ml.y, src + lane, c);
+        }
+        merge();
+        finish();
+      }
+    }
+    __syncthreads();
+    unit += it1 - it0;
+  }
 }
 
 }  // namespace
@@ -338,14 +761,50 @@ hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, hipStream_t s) {
-  const uint64_t blocks = (a.a.n_rows * a.a.n_heads + 3) / 4;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (dtype == GIFT_BF16)
-    k_attention_plain<Bf16><<<(uint32_t)blocks, 256, 0, s>>>(a);
-  else
-    k_attention_plain<F16><<<(uint32_t)blocks, 256, 0, s>>>(a);
+namespace {
+
+template <class E, class S, int MINW>
+hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
+  // as many workgroups as run at once: MINW waves on each SIMD, four SIMDs
+  const uint32_t grid = w.cus * (4 * MINW / S::kWaves);
+  static_assert(4 * MINW % S::kWaves == 0, "whole workgroups");
+  if (2 * grid * S::kPartial > w.partial_bytes || grid > kAttnCounters) return hipErrorInvalidValue;
+  k_tree_attention<E, S, MINW><<<grid, S::kThreads, 0, s>>>(a, w.mem);
   return hipGetLastError();
+}
+
+// Waves that share a tile of keys, by the rows that a request has on average
+// at a KV head.
+template <class E, int D>
+hipError_t attend_by_rows(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
+  const uint64_t rows = a.a.n_reqs ? (a.a.n_rows * a.group + a.a.n_reqs - 1) / a.a.n_reqs : 1;
+  if constexpr (D <= 128) {
+    if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 2>(a, w, s);
+    if (rows <= 64) return attend<E, Shape<D, 2, 4, 1>, 2>(a, w, s);
+    if (rows <= 128) return attend<E, Shape<D, 4, 2, 2>, 2>(a, w, s);
+    return attend<E, Shape<D, 8, 1, 4>, 2>(a, w, s);
+  } else {
+    if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 1>(a, w, s);
+    if (rows <= 64) return attend<E, Shape<D, 2, 2, 1>, 1>(a, w, s);
+    if (rows <= 128) return attend<E, Shape<D, 4, 2, 1>, 2>(a, w, s);
+    return attend<E, Shape<D, 8, 1, 2>, 2>(a, w, s);
+  }
+}
+
+template <class E>
+hipError_t attend_by_dim(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
+  switch (a.kv.head_dim) {
+    case 64: return attend_by_rows<E, 64>(a, w, s);
+    case 96: return attend_by_rows<E, 96>(a, w, s);
+    case 128: return attend_by_rows<E, 128>(a, w, s);
+    default: return attend_by_rows<E, 256>(a, w, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s) {
+  return dtype == GIFT_BF16 ? attend_by_dim<Bf16>(a, w, s) : attend_by_dim<F16>(a, w, s);
 }
 
 }  // namespace gift

@@ -17,7 +17,7 @@ using namespace gift;
 
 struct gift_attention_work_s {
   int device;
-  void* mem;
+  AttnWork w;
 };
 
 namespace {
@@ -193,9 +193,26 @@ gift_status gift_attention_work_create(hipStream_t stream, gift_attention_work* 
   int dev;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return report_hip(e, "hipGetDevice");
-  gift_attention_work w = new (std::nothrow) gift_attention_work_s{dev, nullptr};
+  int cus = 0;
+  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) return report_hip(e, "hipDeviceGetAttribute");
+  if (cus < 1) cus = 1;
+  if (cus > (int)kAttnCounters / 2) cus = kAttnCounters / 2;  // two workgroups a CU at most
+  gift_attention_work w = new (std::nothrow) gift_attention_work_s{dev, {nullptr, (uint32_t)cus, 2 * kAttnPlace * cus}};
   if (!w) return report(GIFT_E_NOMEM, "host memory");
-  (void)stream;
+  const size_t counters = 4ull * kAttnCounters;
+  e = hipMalloc((void**)&w->w.mem, counters + w->w.partial_bytes);
+  if (e != hipSuccess) {
+    delete w;
+    return report_hip(e, "attention workspace");
+  }
+  e = hipMemsetAsync(w->w.mem, 0, counters, stream);
+  if (e == hipSuccess) e = hipStreamSynchronize(stream);
+  if (e != hipSuccess) {
+    (void)hipFree(w->w.mem);
+    delete w;
+    return report_hip(e, "attention workspace");
+  }
   *out = w;
   return GIFT_OK;
 }
@@ -203,8 +220,15 @@ gift_status gift_attention_work_create(hipStream_t stream, gift_attention_work* 
 gift_status gift_attention_work_destroy(gift_attention_work w) {
   clear_error();
   if (!w) return GIFT_OK;
+  int dev;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && dev != w->device) e = hipSetDevice(w->device);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  hipError_t f = hipFree(w->w.mem);
+  if (e == hipSuccess && dev != w->device) e = hipSetDevice(dev);
   delete w;
-  return GIFT_OK;
+  if (e == hipSuccess) e = f;
+  return e == hipSuccess ? GIFT_OK : report_hip(e, "attention workspace");
 }
 
 gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* kv, const gift_kv_format* format,
@@ -262,7 +286,7 @@ gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* k
   if (g.n_rows == 0) return GIFT_OK;
   a.a = g;
   a.group = g.n_heads / a.kv.heads;
-  e = launch_tree_attention(a, format->dtype, stream);
+  e = launch_tree_attention(a, format->dtype, work->w, stream);
   return e == hipSuccess ? GIFT_OK : report_hip(e, "tree_attention");
 }
 

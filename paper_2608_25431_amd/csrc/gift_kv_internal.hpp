@@ -44,6 +44,17 @@ struct AttnArgs {
   gift_tree_attention_args a;
   uint32_t group;  // query heads of a KV head
 };
-hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, hipStream_t s);
+// The attention's workspace: counters of the columns that are joined (zero
+// between calls: the workgroup that joins a column clears its counter), then
+// two places per workgroup for a column's part (at most 8 waves of 32 columns
+// of 256 elements and their maxima and sums).
+constexpr uint32_t kAttnCounters = 16384;
+constexpr size_t kAttnPlace = 8 * (256 * 32 * 4 + 512);
+struct AttnWork {
+  uint8_t* mem;
+  uint32_t cus;
+  size_t partial_bytes;  // past the counters
+};
+hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
 
 }  // namespace gift
