@@ -227,7 +227,10 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 // order, four keys at a time, by the transposing LDS read.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct Bf16 {
@@ -325,7 +328,7 @@ struct State {
     for (int t = 0; t < S::kAcc; t++) o[t] = f32x16{};
   }
   // Adds a state with the whole sum l2 (given to one of the two lanes of a column).
-  __device__ void add(float m2, float l2, const float4* src, float c) {
+  __device__ void add(float m2, float l2, const f32x4* src, float c) {
     const float mn = fmaxf(m, m2), safe = mn == -INFINITY ? 0.f : mn;
     const float f1 = exp2f((m - safe) * c), f2 = exp2f((m2 - safe) * c);
     m = mn;
@@ -334,23 +337,41 @@ struct State {
     for (int t = 0; t < S::kAcc; t++)
 #pragma unroll
       for (int q = 0; q < 4; q++) {
-        const float4 v = src[(t * 4 + q) * kWave];
+        const f32x4 v = src[(t * 4 + q) * kWave];
         o[t][4 * q] = o[t][4 * q] * f1 + v.x * f2;
         o[t][4 * q + 1] = o[t][4 * q + 1] * f1 + v.y * f2;
         o[t][4 * q + 2] = o[t][4 * q + 2] * f1 + v.z * f2;
         o[t][4 * q + 3] = o[t][4 * q + 3] * f1 + v.w * f2;
       }
   }
-  // dst: [kAcc * 4][64] float4, then [64] (m, l)
-  __device__ void put(float4* dst, uint32_t lane) const {
+  // dst: [kAcc * 4][64] f32x4, then [64] (m, l)
+  __device__ void put(f32x4* dst, uint32_t lane) const {
 #pragma unroll
     for (int t = 0; t < S::kAcc; t++)
 #pragma unroll
       for (int q = 0; q < 4; q++)
-        dst[(t * 4 + q) * kWave + lane] = make_float4(o[t][4 * q], o[t][4 * q + 1], o[t][4 * q + 2], o[t][4 * q + 3]);
-    ((float2*)(dst + S::kAcc * 4 * kWave))[lane] = make_float2(m, l);
+        dst[(t * 4 + q) * kWave + lane] = f32x4{o[t][4 * q], o[t][4 * q + 1], o[t][4 * q + 2], o[t][4 * q + 3]};
+    ((f32x2*)(dst + S::kAcc * 4 * kWave))[lane] = f32x2{m, l};
+  }
+  // The same layout in memory that workgroups of other XCDs read: stores and loads of single words at the device's
+  // scope, past the XCDs' own L2s.  A fence would write back and drop the whole L2 instead (with one on each side,
+  // 64 requests of 128-2048 tokens took 185 us longer).
+  __device__ void publish(uint64_t* dst, uint32_t lane) const {
+#pragma unroll
+    for (int t = 0; t < S::kAcc; t++)
+#pragma unroll
+      for (int q = 0; q < 8; q++)
+        __hip_atomic_store(dst + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2,
+                           __builtin_bit_cast(uint64_t, f32x2{o[t][2 * q], o[t][2 * q + 1]}), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(dst + S::kAcc * 8 * kWave + lane, __builtin_bit_cast(uint64_t, f32x2{m, l}), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
   }
 };
+
+__device__ inline f32x2 published(const uint8_t* part, uint32_t at) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)part + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
 
 __device__ inline uint64_t uniform(uint64_t x) {
   return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | __builtin_amdgcn_readfirstlane((uint32_t)x);
@@ -386,8 +407,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     for (uint32_t i = wg; i < loose; i += n_wg) {
       const uint32_t r = i < lo ? i : hi + (i - lo);
       for (uint32_t u = tid; u < a.n_heads * S::kPieces; u += S::kThreads)
-        *(uint4*)((uint8_t*)a.out + r * a.out_row_stride + u / S::kPieces * a.out_head_stride + u % S::kPieces * 16) =
-            make_uint4(0, 0, 0, 0);
+        *(u32x4*)((uint8_t*)a.out + r * a.out_row_stride + u / S::kPieces * a.out_head_stride + u % S::kPieces * 16) =
+            u32x4{0, 0, 0, 0};
       if (a.lse)
         for (uint32_t h = tid; h < a.n_heads; h += S::kThreads) a.lse[(uint64_t)r * a.n_heads + h] = -INFINITY;
     }
@@ -450,6 +471,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   // of the group's TK * 32 rows
   const uint32_t my_row = wq * S::kRowsAtOnce + row_lane % S::kRowsAtOnce + row_lane / S::kRowsAtOnce * (S::kRowsAtOnce * S::WQ);
   const uint32_t piece = lane % S::kLanes, at_once = lane / S::kLanes;
+  // where this lane's first piece of K and of V goes in LDS
+  const uint32_t to_row = wq * S::kRowsAtOnce + at_once,
+                 to_tile = (wk * S::TK + to_row / kTileKeys) * S::kTileBytes + piece * 16,
+                 k_to = to_tile + to_row % kTileKeys * S::kKRow,
+                 v_to = to_tile + kTileKeys * S::kKRow + to_row % kTileKeys * S::kVRow;
   uint32_t* counters = (uint32_t*)work;
   uint8_t* partials = work + 4 * kAttnCounters;
 
@@ -477,8 +503,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         const uint8_t* qp = (const uint8_t*)a.q + qtok * a.q_row_stride + head * a.q_head_stride + half * 16;
 #pragma unroll
         for (int s = 0; s < S::D / 16; s++) {
-          uint4 x = *(const uint4*)(qp + 32 * s);
-          x.x ^= neg, x.y ^= neg, x.z ^= neg, x.w ^= neg;
+          u32x4 x = *(const u32x4*)(qp + 32 * s);
+          x ^= neg;
           q[s] = __builtin_bit_cast(vec, x);
         }
       }
@@ -493,7 +519,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
         return j < r.len ? tab[j >> p.kv.block_shift] : 0u;
       };
-      uint4 kx[S::kLoads], vx[S::kLoads];
+      u32x4 kx[S::kLoads], vx[S::kLoads];
       bool row_ok = false;
       bool drafted = false;  // the round's rows of this wave may hold drafted keys
       // second step: addresses of the rows, handed to the lanes that load them
@@ -518,8 +544,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           const uint8_t *kr = (const uint8_t*)__shfl((unsigned long long)kp, from),
                         *vr = (const uint8_t*)__shfl((unsigned long long)vp, from);
           if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
-            kx[i] = *(const uint4*)(kr + piece * 16);
-            vx[i] = *(const uint4*)(vr + piece * 16);
+            kx[i] = *(const u32x4*)(kr + piece * 16);
+            vx[i] = *(const u32x4*)(vr + piece * 16);
           }
         }
       };
@@ -533,22 +559,21 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           const uint32_t slot = i * S::kRowsAtOnce + at_once;
           bool keep = (oks >> slot) & 1;
           if (drafted) {
-            const uint32_t w[4] = {vx[i].x, vx[i].y, vx[i].z, vx[i].w};
-            bool odd = false;
+                        bool odd = false;
 #pragma unroll
             for (int e = 0; e < 4; e++)
-              odd |= (w[e] & E::kExp) == E::kExp || (w[e] >> 16 & E::kExp) == E::kExp;
+              odd |= (vx[i][e] & E::kExp) == E::kExp || (vx[i][e] >> 16 & E::kExp) == E::kExp;
             const uint64_t odds = __ballot(odd && keep && piece < (uint32_t)S::kPieces);
             const uint64_t lanes = S::kLanes == 64 ? ~0ull : (1ull << (S::kLanes % 64)) - 1;
             if (odds >> (at_once * S::kLanes) & lanes) keep = false;
             if (row_lane / S::kRowsAtOnce == (uint32_t)i && (odds >> (row_lane % S::kRowsAtOnce * S::kLanes) & lanes)) flag |= 2u;
           }
-          const uint32_t row = wq * S::kRowsAtOnce + at_once + i * (S::kRowsAtOnce * S::WQ);
-          uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + row / kTileKeys) * S::kTileBytes;
+          constexpr int kStep = S::kRowsAtOnce * S::WQ;  // a multiple or a divisor of a tile's rows
+          const int tile = i * kStep / kTileKeys, row = i * kStep % kTileKeys;
           if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
-            *(uint4*)(tile + row % kTileKeys * S::kKRow + piece * 16) = kx[i];
-            *(uint4*)(tile + kTileKeys * S::kKRow + row % kTileKeys * S::kVRow + piece * 16) =
-                keep ? vx[i] : make_uint4(0, 0, 0, 0);
+            uint8_t* at = area + buf * (S::kTiles * S::kTileBytes);
+            *(u32x4*)(at + k_to + tile * S::kTileBytes + row * S::kKRow) = kx[i];
+            *(u32x4*)(at + v_to + tile * S::kTileBytes + row * S::kVRow) = keep ? vx[i] : u32x4{0, 0, 0, 0};
           }
         }
         if (lane < (uint32_t)S::kRows) row_flags[buf][wk * S::TK + my_row / kTileKeys][my_row % kTileKeys] = (uint8_t)flag;
@@ -672,66 +697,101 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     }
 
     // the key groups' states meet in the first group
-    auto merge = [&]() {
-      if constexpr (S::WK > 1) {
-        constexpr int kFloat4 = S::kAcc * 4 * kWave + kWave / 2;
-        __syncthreads();
-        if (wk > 0) st.put((float4*)area + (size_t)(wave - S::WQ) * kFloat4, lane);
-        __syncthreads();
-        if (wk == 0) {
+    constexpr size_t kPer = S::kAcc * 4096 + 512;  // bytes of a wave's state
+    if constexpr (S::WK > 1) {
+      __syncthreads();
+      if (wk > 0) st.put((f32x4*)(area + (wave - S::WQ) * kPer), lane);
+      __syncthreads();
+      if (wk == 0) {
 #pragma unroll 1
-          for (int k = 1; k < S::WK; k++) {
-            const float4* src = (const float4*)area + (size_t)((k - 1) * S::WQ + wq) * kFloat4;
-            const float2 ml = ((const float2*)(src + S::kAcc * 4 * kWave))[lane];
-            st.add(ml.x, ml.y, src + lane, c);
-          }
+        for (int k = 1; k < S::WK; k++) {
+          const f32x4* src = (const f32x4*)(area + ((k - 1) * S::WQ + wq) * kPer);
+          const f32x2 ml = ((const f32x2*)(src + S::kAcc * 4 * kWave))[lane];
+          st.add(ml.x, ml.y, src + lane, c);
         }
       }
+    }
+    uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8;
+    auto write = [&](int t, const f32x16& o, float inv) {
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        typedef typename E::elem elem4 __attribute__((ext_vector_type(4)));
+        elem4 x;
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] = (typename E::elem)(o[4 * k + i] * inv);
+        *(elem4*)(op + 64 * t + 16 * k) = x;
+      }
     };
-    merge();
-    auto finish = [&]() {
-      if (wk > 0 || !qlive) return;
-      const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
-      uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8;
-#pragma unroll
-      for (int t = 0; t < S::kAcc; t++)
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-          typename E::elem x[4];
-#pragma unroll
-          for (int i = 0; i < 4; i++) x[i] = (typename E::elem)(st.o[t][4 * k + i] * inv);
-          *(uint2*)(op + 64 * t + 16 * k) = __builtin_bit_cast(uint2, x);
-        }
+    auto write_lse = [&](float m, float l) {
       if (a.lse && half == 0)
-        a.lse[qtok * a.n_heads + head] = st.l == 0.f ? -INFINITY : (st.m * c + log2f(st.l)) * 0.693147181f;
+        a.lse[qtok * a.n_heads + head] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * 0.693147181f;
     };
     const uint32_t w0 = (uint32_t)(((col_first + 1) * n_wg - 1) / total), w1 = (uint32_t)(((col_last + 1) * n_wg - 1) / total);
     if (w0 == w1) {
-      finish();
+      if (wk == 0 && qlive) {
+        const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+#pragma unroll
+        for (int t = 0; t < S::kAcc; t++) write(t, st.o[t], inv);
+        write_lse(st.m, st.l);
+      }
     } else {
       // of a workgroup's parts at most the first joins a column begun before it, and at most the last one begins a
       // column that others end: two places each
-      const uint32_t place = 2 * wg + (wg == w0 ? 1 : 0);
-      if (wk == 0) st.put((float4*)(partials + place * S::kPartial) + (size_t)wq * (S::kAcc * 4 * kWave + kWave / 2), lane);
-      __threadfence();
+      if (wk == 0 && qlive)
+        st.publish((uint64_t*)(partials + (2 * wg + (wg == w0 ? 1 : 0)) * S::kPartial + wq * kPer), lane);
+      __builtin_amdgcn_s_waitcnt(0);  // the stores have arrived before the count goes up
       __syncthreads();
       if (tid == 0) {
-        const uint32_t parts = w1 - w0 + 1, before = atomicAdd(&counters[w0], 1u);
+        const uint32_t parts = w1 - w0 + 1,
+                       before = __hip_atomic_fetch_add(&counters[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         last_one = before == parts - 1;
-        if (before == parts - 1) atomicExch(&counters[w0], 0u);  // clear for the next call
+        if (before == parts - 1)  // clear for the next call
+          __hip_atomic_store(&counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
-      if (last_one) {
-        __threadfence();
-        st.clear();
-        for (uint32_t w = w0 + wk; w <= w1; w += S::WK) {
-          const float4* src = (const float4*)(partials + (2 * w + (w == w0 ? 1 : 0)) * S::kPartial) +
-                              (size_t)wq * (S::kAcc * 4 * kWave + kWave / 2);
-          const float2 ml = ((const float2*)(src + S::kAcc * 4 * kWave))[lane];
-          st.add(ml.x, ml.y, src + lane, c);
+      if (last_one && qlive) {
+        // The parts' maxima and sums first, then their outputs, a group of waves every WK-th 32 elements: the loads of
+        // kAhead parts are in flight at a time.
+        constexpr uint32_t kAhead = 8;
+        auto part = [&](uint32_t w) { return partials + (2 * w + (w == w0 ? 1 : 0)) * S::kPartial + wq * kPer; };
+        float m = -INFINITY, l = 0;
+        for (uint32_t w = w0; w <= w1; w += kAhead) {
+          f32x2 ml[kAhead];
+#pragma unroll
+          for (uint32_t u = 0; u < kAhead; u++) ml[u] = published(part(w + u <= w1 ? w + u : w1), S::kAcc * 8 * kWave + lane);
+          float mn = m;
+#pragma unroll
+          for (uint32_t u = 0; u < kAhead; u++) mn = fmaxf(mn, ml[u][0]);
+          const float safe = mn == -INFINITY ? 0.f : mn;
+          l *= exp2f((m - safe) * c);
+          m = mn;
+#pragma unroll
+          for (uint32_t u = 0; u < kAhead; u++)
+            if (w + u <= w1) l += ml[u][1] * exp2f((ml[u][0] - safe) * c);
         }
-        merge();
-        finish();
+        const float safe = m == -INFINITY ? 0.f : m, inv = l == 0.f ? 0.f : 1.f / l;
+        for (uint32_t t = wk; t < (uint32_t)S::kAcc; t += S::WK) {
+          f32x16 o = f32x16{};
+          for (uint32_t w = w0; w <= w1; w += kAhead / 2) {
+            f32x2 x[kAhead / 2][8], ml[kAhead / 2];
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead / 2; u++) {
+              const uint8_t* from = part(w + u <= w1 ? w + u : w1);
+              ml[u] = published(from, S::kAcc * 8 * kWave + lane);
+#pragma unroll
+              for (int q = 0; q < 8; q++) x[u][q] = published(from, ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead / 2; u++) {
+              if (w + u > w1) break;
+              const float f = exp2f((ml[u][0] - safe) * c);
+#pragma unroll
+              for (int i = 0; i < 16; i++) o[i] += x[u][i / 2][i % 2] * f;
+            }
+          }
+          write(t, o, inv);
+        }
+        if (wk == 0) write_lse(m, l);
       }
     }
     __syncthreads();
@@ -778,16 +838,14 @@ hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
 template <class E, int D>
 hipError_t attend_by_rows(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
   const uint64_t rows = a.a.n_reqs ? (a.a.n_rows * a.group + a.a.n_reqs - 1) / a.a.n_reqs : 1;
+  if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 1>(a, w, s);
   if constexpr (D <= 128) {
-    if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 2>(a, w, s);
     if (rows <= 64) return attend<E, Shape<D, 2, 4, 1>, 2>(a, w, s);
     if (rows <= 128) return attend<E, Shape<D, 4, 2, 2>, 2>(a, w, s);
     return attend<E, Shape<D, 8, 1, 4>, 2>(a, w, s);
   } else {
-    if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 1>(a, w, s);
     if (rows <= 64) return attend<E, Shape<D, 2, 2, 1>, 1>(a, w, s);
-    if (rows <= 128) return attend<E, Shape<D, 4, 2, 1>, 2>(a, w, s);
-    return attend<E, Shape<D, 8, 1, 2>, 2>(a, w, s);
+    return attend<E, Shape<D, 4, 1, 2>, 1>(a, w, s);
   }
 }
 
