@@ -281,6 +281,7 @@ struct Shape {
   static constexpr int kLoads = kTileKeys * TK / (kRowsAtOnce * WQ);  // 16-byte loads of K (and of V) per lane and round
   static constexpr int kRows = kRowsAtOnce * kLoads;                  // rows that a wave loads in a round
   static constexpr int kAcc = D / 32;
+  static constexpr bool kQueriesInLds = WQ == 1;
   static constexpr int kTileArea = kBufs * kTiles * kTileBytes, kMergeArea = (kWaves - WQ) * (kAcc * 4096 + 512);
   static constexpr int kArea = kTileArea > kMergeArea ? kTileArea : kMergeArea;
   static constexpr size_t kPartial = (size_t)WQ * (kAcc * 4096 + 512);
@@ -312,6 +313,16 @@ __device__ Req req_of(const AttnArgs& p, uint32_t b) {
   r.rounds = r.dead || rounds == 0 ? 1 : rounds;
   r.col_tiles = (uint32_t)(((uint64_t)r.rows * p.group + 32 * S::WQ - 1) / (32 * S::WQ));
   r.cols = r.col_tiles * p.kv.heads;
+  return r;
+}
+
+// The same for every lane: held in scalar registers, which the compiler does not see by itself.
+template <class S>
+__device__ Req uniform_req_of(const AttnArgs& p, uint32_t b) {
+  Req r = req_of<S>(p, b);
+  for (uint32_t* x : {&r.row0, &r.rows, &r.len, &r.ctx_tiles, &r.tiles, &r.rounds, &r.cols, &r.col_tiles})
+    *x = __builtin_amdgcn_readfirstlane(*x);
+  r.dead = __builtin_amdgcn_readfirstlane(r.dead);
   return r;
 }
 
@@ -377,6 +388,19 @@ __device__ inline uint64_t uniform(uint64_t x) {
   return (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | __builtin_amdgcn_readfirstlane((uint32_t)x);
 }
 
+// x, worked out here: without it the compiler keeps what it can derive from a lane's number in a register for each use
+// across the loop over the keys, and spills the operands.
+__device__ inline uint32_t fresh(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ inline const uint8_t* pointer_of(const uint8_t* p, uint32_t lane) {
+  const uint32_t lo = __builtin_amdgcn_ds_bpermute(4 * lane, (uint32_t)(uintptr_t)p),
+                 hi = __builtin_amdgcn_ds_bpermute(4 * lane, (uint32_t)((uintptr_t)p >> 32));
+  return (const uint8_t*)((uint64_t)hi << 32 | lo);
+}
+
 __device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
 
 // Work is cut evenly: a round (kTiles tiles of 32 keys) of a column tile (32 WQ
@@ -389,6 +413,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   typedef typename E::vec vec;
   const gift_tree_attention_args& a = p.a;
   __shared__ __align__(16) uint8_t area[S::kArea];
+  __shared__ __align__(16) uint8_t queries[S::kQueriesInLds ? 32 * S::kKRow : 16];
   __shared__ uint8_t row_flags[S::kBufs][S::kTiles][kTileKeys];  // bit 0: the key exists, bit 1: its V is not finite
   __shared__ uint64_t sums[S::kWaves];
   __shared__ uint64_t found[2];
@@ -471,6 +496,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   // of the group's TK * 32 rows
   const uint32_t my_row = wq * S::kRowsAtOnce + row_lane % S::kRowsAtOnce + row_lane / S::kRowsAtOnce * (S::kRowsAtOnce * S::WQ);
   const uint32_t piece = lane % S::kLanes, at_once = lane / S::kLanes;
+  const uint32_t read_at = 16 * (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces ? piece : 0);
   // where this lane's first piece of K and of V goes in LDS
   const uint32_t to_row = wq * S::kRowsAtOnce + at_once,
                  to_tile = (wk * S::TK + to_row / kTileKeys) * S::kTileBytes + piece * 16,
@@ -479,11 +505,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   uint32_t* counters = (uint32_t*)work;
   uint8_t* partials = work + 4 * kAttnCounters;
 
-  Req r = req_of<S>(p, b);
+  Req r = uniform_req_of<S>(p, b);
   while (unit < unit_end) {
     while (unit >= base + (uint64_t)r.cols * r.rounds) {
       base += (uint64_t)r.cols * r.rounds;
-      r = req_of<S>(p, ++b);
+      r = uniform_req_of<S>(p, ++b);
     }
     const uint32_t at = (uint32_t)(unit - base), column = at / r.rounds, it0 = at % r.rounds;
     const uint64_t col_first = unit - it0, col_last = col_first + r.rounds - 1;
@@ -498,15 +524,20 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     State<S> st;
     st.clear();
     if (!r.dead && r.tiles) {
-      vec q[S::D / 16];
-      {
+      // Queries: in registers, or in LDS where all waves have the same ones and need the registers for keys on their way.
+      vec q[S::kQueriesInLds ? 1 : S::D / 16];
+      if constexpr (S::kQueriesInLds) {
+        for (uint32_t u = tid; u < 32 * S::kPieces; u += S::kThreads) {
+          const uint32_t line = u / S::kPieces, row = ct * 32 + line < rows ? ct * 32 + line : 0, tok = row / p.group;
+          const uint8_t* qp = (const uint8_t*)a.q + (uint64_t)(r.row0 + tok) * a.q_row_stride +
+                              (uint64_t)(g * p.group + (row - tok * p.group)) * a.q_head_stride;
+          *(u32x4*)(queries + line * S::kKRow + u % S::kPieces * 16) = *(const u32x4*)(qp + u % S::kPieces * 16) ^ neg;
+        }
+        __syncthreads();
+      } else {
         const uint8_t* qp = (const uint8_t*)a.q + qtok * a.q_row_stride + head * a.q_head_stride + half * 16;
 #pragma unroll
-        for (int s = 0; s < S::D / 16; s++) {
-          u32x4 x = *(const u32x4*)(qp + 32 * s);
-          x ^= neg;
-          q[s] = __builtin_bit_cast(vec, x);
-        }
+        for (int s = 0; s < S::D / 16; s++) q[s] = __builtin_bit_cast(vec, *(const u32x4*)(qp + 32 * s) ^ neg);
       }
       const uint32_t* tab = a.tables + b * a.table_stride;
       const uint8_t* kbase = p.kv.base + a.layer * p.kv.layer_stride + g * p.kv.head_stride;
@@ -514,68 +545,77 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
                     *dv = (const uint8_t*)a.v + r.row0 * a.v_row_stride + g * a.v_head_stride;
       const uint32_t ctx_keys = r.ctx_tiles * kTileKeys;
 
-      // first step of a round's loads: the block id of this lane's row
+      // Loads of a round, first step: the block id of this lane's row.  It is asked for two rounds ahead and before the
+      // rows of the round between, since loads come back in order and the addresses wait for it.
       auto block_of = [&](uint32_t it) -> uint32_t {
         const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
-        return j < r.len ? tab[j >> p.kv.block_shift] : 0u;
+        return *(it < it1 && j < r.len ? tab + (j >> p.kv.block_shift) : a.row_begin);  // no branch around the load
       };
-      u32x4 kx[S::kLoads], vx[S::kLoads];
-      bool row_ok = false;
-      bool drafted = false;  // the round's rows of this wave may hold drafted keys
-      // second step: addresses of the rows, handed to the lanes that load them
-      auto load = [&](uint32_t it, uint32_t id) {
+      // Second step: this lane's row.
+      struct Row {
+        const uint8_t *k, *v;
+        bool ok;       // it exists
+        bool drafted;  // the round's rows of this wave may hold drafted keys
+      };
+      auto row_of = [&](uint32_t it, uint32_t id) -> Row {
         const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
-        const uint8_t *kp, *vp;
-        if (j < ctx_keys) {
-          row_ok = j < r.len && id < p.kv.n_blocks;
-          kp = kbase + id * p.kv.block_stride + (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride;
-          vp = kp + p.kv.v_off;
-        } else {
+        Row x;
+        x.drafted = (it * S::kTiles + wk * S::TK + S::TK) * kTileKeys > ctx_keys;
+        x.k = kbase + id * p.kv.block_stride + (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride;
+        x.v = x.k + p.kv.v_off;
+        x.ok = it < it1 && j < r.len && id < p.kv.n_blocks;
+        if (x.drafted && j >= ctx_keys) {
           const uint32_t t = j - ctx_keys;
-          row_ok = a.k && t < r.rows;
-          kp = dk + t * a.k_row_stride;
-          vp = dv + t * a.v_row_stride;
+          x.ok = it < it1 && a.k && t < r.rows;
+          x.k = dk + t * a.k_row_stride;
+          x.v = dv + t * a.v_row_stride;
         }
-        if (!row_ok) kp = vp = (const uint8_t*)a.q;  // any row that may be read: nothing of it is used
-        drafted = (it * S::kTiles + wk * S::TK + S::TK) * kTileKeys > ctx_keys;
+        if (!x.ok) x.k = x.v = (const uint8_t*)a.q;  // a row that may be read, of which nothing is used
+        return x;
+      };
+      // Third step: the rows' pieces, each lane from the address that another lane worked out.
+      auto fetch = [&](u32x4 (&x)[S::kLoads], const uint8_t* rows) {
+        const uint32_t first = fresh(at_once);
 #pragma unroll
         for (int i = 0; i < S::kLoads; i++) {
-          const int from = i * S::kRowsAtOnce + at_once;
-          const uint8_t *kr = (const uint8_t*)__shfl((unsigned long long)kp, from),
-                        *vr = (const uint8_t*)__shfl((unsigned long long)vp, from);
-          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
-            kx[i] = *(const u32x4*)(kr + piece * 16);
-            vx[i] = *(const u32x4*)(vr + piece * 16);
-          }
+          const uint8_t* from = pointer_of(rows, i * S::kRowsAtOnce + first);
+          x[i] = *(const u32x4*)(from + read_at);
         }
       };
-      // third step: into LDS.  V rows of keys that do not exist, and drafted ones that are not finite, are stored as
-      // zeros: a weight of zero times NaN would reach every row.
-      auto store = [&](uint32_t buf) {
-        uint32_t flag = row_ok ? 1u : 0u;
-        const uint64_t oks = __ballot(row_ok);
+      // Fourth step: into LDS.
+      constexpr int kStep = S::kRowsAtOnce * S::WQ;  // rows from one load to the next: a multiple or a divisor of a tile's
+      auto store_k = [&](const u32x4 (&x)[S::kLoads], uint32_t buf) {
+        uint8_t* at = area + buf * (S::kTiles * S::kTileBytes) + fresh(k_to);
 #pragma unroll
-        for (int i = 0; i < S::kLoads; i++) {
-          const uint32_t slot = i * S::kRowsAtOnce + at_once;
-          bool keep = (oks >> slot) & 1;
-          if (drafted) {
-                        bool odd = false;
+        for (int i = 0; i < S::kLoads; i++)
+          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces)
+            *(u32x4*)(at + i * kStep / kTileKeys * S::kTileBytes + i * kStep % kTileKeys * S::kKRow) = x[i];
+      };
+      // V rows of keys that do not exist, and drafted ones that are not finite, are stored as zeros: a weight of zero
+      // times NaN would reach every row.
+      auto store_v = [&](u32x4 (&x)[S::kLoads], const Row& row, uint32_t buf) {
+        uint32_t flag = row.ok ? 1u : 0u;
+        const uint64_t oks = __ballot(row.ok);
+        if (oks != ~0ull || row.drafted) {
+          const uint32_t first = fresh(at_once), own = fresh(row_lane);
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-              odd |= (vx[i][e] & E::kExp) == E::kExp || (vx[i][e] >> 16 & E::kExp) == E::kExp;
-            const uint64_t odds = __ballot(odd && keep && piece < (uint32_t)S::kPieces);
-            const uint64_t lanes = S::kLanes == 64 ? ~0ull : (1ull << (S::kLanes % 64)) - 1;
-            if (odds >> (at_once * S::kLanes) & lanes) keep = false;
-            if (row_lane / S::kRowsAtOnce == (uint32_t)i && (odds >> (row_lane % S::kRowsAtOnce * S::kLanes) & lanes)) flag |= 2u;
-          }
-          constexpr int kStep = S::kRowsAtOnce * S::WQ;  // a multiple or a divisor of a tile's rows
-          const int tile = i * kStep / kTileKeys, row = i * kStep % kTileKeys;
-          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces) {
-            uint8_t* at = area + buf * (S::kTiles * S::kTileBytes);
-            *(u32x4*)(at + k_to + tile * S::kTileBytes + row * S::kKRow) = kx[i];
-            *(u32x4*)(at + v_to + tile * S::kTileBytes + row * S::kVRow) = keep ? vx[i] : u32x4{0, 0, 0, 0};
+          for (int i = 0; i < S::kLoads; i++) {
+            bool keep = oks >> (i * S::kRowsAtOnce + first) & 1;
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; e++) odd |= (x[i][e] & E::kExp) == E::kExp || (x[i][e] >> 16 & E::kExp) == E::kExp;
+            const uint64_t odds = __ballot(row.drafted && odd && keep && piece < (uint32_t)S::kPieces);
+            constexpr uint64_t kOneRow = (1ull << S::kLanes) - 1;
+            if (odds >> (first * S::kLanes) & kOneRow) keep = false;
+            if (own / S::kRowsAtOnce == (uint32_t)i && (odds >> (own % S::kRowsAtOnce * S::kLanes) & kOneRow)) flag |= 2u;
+            if (!keep) x[i] = u32x4{0, 0, 0, 0};
           }
         }
+        uint8_t* at = area + buf * (S::kTiles * S::kTileBytes) + fresh(v_to);
+#pragma unroll
+        for (int i = 0; i < S::kLoads; i++)
+          if (S::kPieces == S::kLanes || piece < (uint32_t)S::kPieces)
+            *(u32x4*)(at + i * kStep / kTileKeys * S::kTileBytes + i * kStep % kTileKeys * S::kVRow) = x[i];
         if (lane < (uint32_t)S::kRows) row_flags[buf][wk * S::TK + my_row / kTileKeys][my_row % kTileKeys] = (uint8_t)flag;
       };
       auto meet = [&]() {
@@ -586,112 +626,157 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           __syncthreads();
         }
       };
-      auto compute = [&](uint32_t it, uint32_t buf) {
-#pragma unroll 1
-        for (int s = 0; s < S::TK; s++) {
-          const uint32_t t = it * S::kTiles + wk * S::TK + s;
-          if (t >= r.tiles) break;
-          const uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + s) * S::kTileBytes;
-          const uint32_t flag = row_flags[buf][wk * S::TK + s][col];
-          const bool draft = t >= r.ctx_tiles;
-          uint32_t see = ~0u;
-          if (draft) {
-            const uint32_t w = t - r.ctx_tiles;
-            if (a.mask)
-              see = w < a.mask_words ? a.mask[qtok * a.mask_words + w] : 0u;
-            else
-              see = token >= 32 * w + 31 ? ~0u : token < 32 * w ? 0u : (2u << (token - 32 * w)) - 1;
-          }
-          f32x16 sc = f32x16{};
-          const uint8_t* krow = tile + col * S::kKRow + half * 16;
+      auto scores = [&](const uint8_t* tile) -> f32x16 {
+        f32x16 sc = f32x16{};
+        const uint8_t* krow = tile + col * S::kKRow + half * 16;
 #pragma unroll
-          for (int d = 0; d < S::D / 16; d++) sc = E::mfma(*(const vec*)(krow + 32 * d), q[d], sc);
-          const uint32_t have = (uint32_t)__ballot(flag & 1);
-          see &= have;
-          const bool part = draft || have != ~0u;
-          if (part) {
+        for (int d = 0; d < S::D / 16; d++)
+          sc = E::mfma(*(const vec*)(krow + 32 * d),
+                       S::kQueriesInLds ? *(const vec*)(queries + col * S::kKRow + half * 16 + 32 * d) : q[S::kQueriesInLds ? 0 : d], sc);
+        return sc;
+      };
+      auto seen = [&](uint32_t see, int i) -> bool { return see >> (8 * (i / 4) + i % 4) & 1; };  // of see >> 4 half
+      // weights of a tile's keys, from their scores and flags
+      auto weigh = [&](f32x16 sc, uint32_t t, uint32_t flag, vec (&w)[2][E::kParts]) {
+        const uint32_t have = (uint32_t)__ballot(flag & 1);
+        const bool draft = t >= r.ctx_tiles;
+        uint32_t see = have;
+        if (draft) {
+          const uint32_t word = t - r.ctx_tiles;
+          if (a.mask)
+            see &= word < a.mask_words ? a.mask[qtok * a.mask_words + word] : 0u;
+          else
+            see &= token >= 32 * word + 31 ? ~0u : token < 32 * word ? 0u : (2u << (token - 32 * word)) - 1;
+        }
+        const bool part = draft || have != ~0u;
+        const uint32_t mine = see >> (4 * half);
+        if (part) {
 #pragma unroll
-            for (int i = 0; i < 16; i++)
-              if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1)) sc[i] = -INFINITY;
-          }
-          float top = sc[0];
+          for (int i = 0; i < 16; i++)
+            if (!seen(mine, i)) sc[i] = -INFINITY;
+        }
+        float top = sc[0];
 #pragma unroll
-          for (int i = 1; i < 16; i++) top = fmaxf(top, sc[i]);
-          top = fmaxf(top, other_half(top));
-          const float mn = fmaxf(st.m, top), safe = mn == -INFINITY ? 0.f : mn;
-          if (__any(mn != st.m)) {
-            const float f = exp2f((st.m - safe) * c);
-            st.l *= f;
+        for (int i = 1; i < 16; i++) top = fmaxf(top, sc[i]);
+        top = fmaxf(top, other_half(top));
+        const float mn = fmaxf(st.m, top), safe = mn == -INFINITY ? 0.f : mn;
+        if (__any(mn != st.m)) {
+          const float f = exp2f((st.m - safe) * c);
+          st.l *= f;
 #pragma unroll
-            for (int d = 0; d < S::kAcc; d++) st.o[d] *= f;
-            st.m = mn;
-          }
-          const float shift = -safe * c;
+          for (int d = 0; d < S::kAcc; d++) st.o[d] *= f;
+          st.m = mn;
+        }
+        const float shift = -safe * c;
 #pragma unroll
-          for (int i = 0; i < 16; i++) sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], c, shift));
-          if (part) {
+        for (int i = 0; i < 16; i++) sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], c, shift));
+        if (part) {
 #pragma unroll
-            for (int i = 0; i < 16; i++)
-              if (!(see >> (8 * (i / 4) + 4 * half + i % 4) & 1)) sc[i] = 0.f;
-          }
+          for (int i = 0; i < 16; i++)
+            if (!seen(mine, i)) sc[i] = 0.f;
+        }
 #pragma unroll
-          for (int i = 0; i < 16; i++) st.l += sc[i];
-          // weights to the operands' type; the sum above is not rounded
-          vec w[2][E::kParts];
-          E::parts(sc, 0, w[0]);
-          E::parts(sc, 1, w[1]);
-          const uint8_t* vrow = tile + kTileKeys * S::kKRow + (4 * half + lane % 16 / 4) * S::kVRow + (lane / 16 % 2 * 16 + lane % 4 * 4) * 2;
+        for (int i = 0; i < 16; i++) st.l += sc[i];
+        // to the operands' type; the sum above is not rounded
+        E::parts(sc, 0, w[0]);
+        E::parts(sc, 1, w[1]);
+        uint32_t odd = draft ? (uint32_t)__ballot(flag & 2) : 0u;
+        while (odd) {  // drafted keys whose V is not finite: only for the rows that see them
+          const uint32_t key = __builtin_ctz(odd);
+          odd &= odd - 1;
+          float own = 0;
 #pragma unroll
-          for (int d = 0; d < S::kAcc; d++)
+          for (int i = 0; i < 16; i++)
+            if ((uint32_t)(8 * (i / 4) + i % 4) == (key & ~4u)) own = sc[i];
+          const float theirs = other_half(own), weight = (key >> 2 & 1) == half ? own : theirs;
+          const typename E::elem* vp =
+              (const typename E::elem*)(dv + (uint64_t)((t - r.ctx_tiles) * kTileKeys + key) * a.v_row_stride);
+          if (see >> key & 1) {
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-              typedef __attribute__((address_space(3))) s16x4 lds4;
-              union {
-                s16x4 x[2];
-                vec v;
-              } u;
-              u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 16 * k * S::kVRow + 64 * d));
-              u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + (16 * k + 8) * S::kVRow + 64 * d));
+            for (int d = 0; d < S::kAcc; d++)
 #pragma unroll
-              for (int e = 0; e < E::kParts; e++) st.o[d] = E::mfma(u.v, w[k][e], st.o[d]);
-            }
-          uint32_t odd = draft ? (uint32_t)__ballot(flag & 2) : 0u;
-          if (odd) {  // drafted keys whose V is not finite: only for the rows that see them
-            while (odd) {
-              const uint32_t key = __builtin_ctz(odd);
-              odd &= odd - 1;
-              float mine = 0;
-#pragma unroll
-              for (int i = 0; i < 16; i++)
-                if ((uint32_t)(8 * (i / 4) + i % 4) == (key & ~4u)) mine = sc[i];
-              const float theirs = other_half(mine), weight = (key >> 2 & 1) == half ? mine : theirs;
-              const typename E::elem* vp = (const typename E::elem*)(dv + (uint64_t)((t - r.ctx_tiles) * kTileKeys + key) * a.v_row_stride);
-              if (see >> key & 1) {
-#pragma unroll
-                for (int d = 0; d < S::kAcc; d++)
-#pragma unroll
-                  for (int i = 0; i < 16; i++) st.o[d][i] += weight * (float)vp[32 * d + 8 * (i / 4) + 4 * half + i % 4];
-              }
-            }
+              for (int i = 0; i < 16; i++) st.o[d][i] += weight * (float)vp[32 * d + 8 * (i / 4) + 4 * half + i % 4];
           }
         }
       };
+      auto add_values = [&](const uint8_t* tile, const vec (&w)[2][E::kParts]) {
+        const uint8_t* vrow = tile + kTileKeys * S::kKRow + (4 * half + lane % 16 / 4) * S::kVRow +
+                              (lane / 16 % 2 * 16 + lane % 4 * 4) * 2;
+#pragma unroll
+        for (int d = 0; d < S::kAcc; d++)
+#pragma unroll
+          for (int k = 0; k < 2; k++) {
+            typedef __attribute__((address_space(3))) s16x4 lds4;
+            union {
+              s16x4 x[2];
+              vec v;
+            } u;
+            u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 16 * k * S::kVRow + 64 * d));
+            u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + (16 * k + 8) * S::kVRow + 64 * d));
+#pragma unroll
+            for (int e = 0; e < E::kParts; e++) st.o[d] = E::mfma(u.v, w[k][e], st.o[d]);
+          }
+      };
 
-      uint32_t id = block_of(it0);
-      load(it0, id);
-      id = it0 + 1 < it1 ? block_of(it0 + 1) : 0u;
-      store(0);
-      meet();
-      for (uint32_t it = it0; it < it1; it++) {
-        const uint32_t buf = S::kBufs == 1 ? 0 : (it - it0) & 1;
-        const bool more = it + 1 < it1;
-        if (more) {
-          load(it + 1, id);
-          id = it + 2 < it1 ? block_of(it + 2) : 0u;
+      if constexpr (S::WQ == 1) {
+        // A tile of the wave's own a round.  One set of registers brings K of the next tile while V of this one is in
+        // use, and V while K is.
+        static_assert(S::TK == 1, "a tile a round");
+        u32x4 x[S::kLoads];
+        const uint8_t* tile = area + wk * S::kTileBytes;
+        uint32_t id = block_of(it0), next = block_of(it0 + 1);
+        Row row = row_of(it0, id);
+        fetch(x, row.k);
+        store_k(x, 0);
+        fetch(x, row.v);
+        for (uint32_t it = it0; it < it1; it++) {
+          id = next;
+          next = block_of(it + 2);
+          const uint32_t t = it * S::kTiles + wk;
+          vec w[2][E::kParts];
+          meet();
+          const f32x16 sc = scores(tile);
+          store_v(x, row, 0);
+          row = row_of(it + 1, id);
+          fetch(x, row.k);
+          meet();
+          weigh(sc, t, row_flags[0][wk][col], w);
+          add_values(tile, w);
+          meet();
+          store_k(x, 0);
+          fetch(x, row.v);
         }
-        if (wave_live) compute(it, buf);
-        if (more) store(S::kBufs == 1 ? 0 : buf ^ 1);
-        meet();
+      } else {
+        u32x4 xk[S::kLoads], xv[S::kLoads];
+        uint32_t id = block_of(it0), next = block_of(it0 + 1);
+        Row row = row_of(it0, id);
+        fetch(xk, row.k);
+        fetch(xv, row.v);
+        for (uint32_t it = it0;; it++) {
+          const uint32_t buf = (it - it0) & 1;
+          store_k(xk, buf);
+          store_v(xv, row, buf);
+          if (it + 1 < it1) {
+            id = next;
+            next = block_of(it + 2);
+            row = row_of(it + 1, id);
+            fetch(xk, row.k);
+            fetch(xv, row.v);
+          }
+          meet();
+          if (wave_live) {
+#pragma unroll 1
+            for (int s = 0; s < S::TK; s++) {
+              const uint32_t t = it * S::kTiles + wk * S::TK + s;
+              if (t >= r.tiles) break;
+              const uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + s) * S::kTileBytes;
+              vec w[2][E::kParts];
+              weigh(scores(tile), t, row_flags[buf][wk * S::TK + s][col], w);
+              add_values(tile, w);
+            }
+          }
+          if (it + 1 == it1) break;
+        }
       }
       st.l += other_half(st.l);
     }
@@ -838,7 +923,7 @@ hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
 template <class E, int D>
 hipError_t attend_by_rows(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
   const uint64_t rows = a.a.n_reqs ? (a.a.n_rows * a.group + a.a.n_reqs - 1) / a.a.n_reqs : 1;
-  if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, 1>(a, w, s);
+  if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, D <= 128 ? 2 : 1>(a, w, s);
   if constexpr (D <= 128) {
     if (rows <= 64) return attend<E, Shape<D, 2, 4, 1>, 2>(a, w, s);
     if (rows <= 128) return attend<E, Shape<D, 4, 2, 2>, 2>(a, w, s);
