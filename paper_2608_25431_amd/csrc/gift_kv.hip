@@ -282,33 +282,52 @@ struct Shape {
   static constexpr int kRows = kRowsAtOnce * kLoads;                  // rows that a wave loads in a round
   static constexpr int kAcc = D / 32;
   static constexpr bool kQueriesInLds = WQ == 1;
-  static constexpr int kTileArea = kBufs * kTiles * kTileBytes, kMergeArea = (kWaves - WQ) * (kAcc * 4096 + 512);
+  // 64 requests stay in registers, four a lane; otherwise the next one is loaded when its turn comes, which shows less
+  // where a column takes longer
+  static constexpr bool kKeepsRequests = WQ == 1 && D <= 128;
+  static constexpr int kTileArea = kBufs * kTiles * kTileBytes, kMergeArea = kWaves * (kAcc * 4096 + 512);
   static constexpr int kArea = kTileArea > kMergeArea ? kTileArea : kMergeArea;
-  static constexpr size_t kPartial = (size_t)WQ * (kAcc * 4096 + 512);
+  static constexpr size_t kPartial = (size_t)WQ * (kAcc * 4096 + 1024);
   static_assert(kLoads >= 1 && kRows <= kWave, "rows of a round");
 };
+
+// What a request's arrays say, cut to the buffers.
+struct Said {
+  uint32_t row0, rows, len;
+  uint32_t dead;  // rejected: zeros
+};
+
+__device__ inline Said said_of(const AttnArgs& p, uint32_t b) {
+  const gift_tree_attention_args& a = p.a;
+  // loads without a branch between them, so that they are on their way together
+  const uint32_t at = b < a.n_reqs ? b : a.n_reqs - 1;
+  const uint32_t r0 = a.row_begin[at], r1 = a.row_begin[at + 1], len = a.lens[at];
+  const uint32_t verdict = (a.verdicts ? (const uint32_t*)a.verdicts : a.lens)[at];
+  const uint32_t total = (uint32_t)a.n_rows, most = a.table_width << p.kv.block_shift;
+  Said s;
+  s.row0 = r0 < total ? r0 : total;
+  const uint32_t end = r1 < total ? r1 : total;
+  s.rows = b < a.n_reqs && end > s.row0 ? end - s.row0 : 0;
+  s.len = len < most ? len : most;
+  s.dead = a.verdicts && verdict != GIFT_SEG_OK;
+  return s;
+}
 
 // A request as the kernel works on it.
 struct Req {
   uint32_t row0, rows, len, ctx_tiles, tiles, rounds, cols, col_tiles;
-  bool dead;  // rejected: zeros
+  bool dead;
 };
 
 template <class S>
-__device__ Req req_of(const AttnArgs& p, uint32_t b) {
-  const gift_tree_attention_args& a = p.a;
+__device__ inline Req req_of(const AttnArgs& p, const Said& s) {
   Req r;
-  const uint32_t total = (uint32_t)a.n_rows;
-  uint32_t lo = a.row_begin[b], hi = a.row_begin[b + 1];
-  lo = lo < total ? lo : total;
-  hi = hi < total ? hi : total;
-  r.row0 = lo;
-  r.rows = hi > lo ? hi - lo : 0;
-  const uint32_t most = a.table_width << p.kv.block_shift, len = a.lens[b];
-  r.len = len < most ? len : most;
-  r.dead = a.verdicts && a.verdicts[b] != GIFT_SEG_OK;
+  r.row0 = s.row0;
+  r.rows = s.rows;
+  r.len = s.len;
+  r.dead = s.dead;
   r.ctx_tiles = (r.len + kTileKeys - 1) / kTileKeys;
-  r.tiles = r.ctx_tiles + (a.k ? (r.rows + kTileKeys - 1) / kTileKeys : 0);
+  r.tiles = r.ctx_tiles + (p.a.k ? (r.rows + kTileKeys - 1) / kTileKeys : 0);
   const uint32_t rounds = (r.tiles + S::kTiles - 1) / S::kTiles;
   r.rounds = r.dead || rounds == 0 ? 1 : rounds;
   r.col_tiles = (uint32_t)(((uint64_t)r.rows * p.group + 32 * S::WQ - 1) / (32 * S::WQ));
@@ -316,14 +335,33 @@ __device__ Req req_of(const AttnArgs& p, uint32_t b) {
   return r;
 }
 
-// The same for every lane: held in scalar registers, which the compiler does not see by itself.
 template <class S>
-__device__ Req uniform_req_of(const AttnArgs& p, uint32_t b) {
-  Req r = req_of<S>(p, b);
-  for (uint32_t* x : {&r.row0, &r.rows, &r.len, &r.ctx_tiles, &r.tiles, &r.rounds, &r.cols, &r.col_tiles})
-    *x = __builtin_amdgcn_readfirstlane(*x);
-  r.dead = __builtin_amdgcn_readfirstlane(r.dead);
+__device__ inline uint64_t units_of(const AttnArgs& p, const Said& s) {
+  const Req r = req_of<S>(p, s);
+  return (uint64_t)r.cols * r.rounds;
+}
+
+// Request b0 + i in scalar registers, of the 64 that a wave's lanes hold.
+template <class S>
+__device__ inline Req req_at(const AttnArgs& p, const Said& s, uint32_t i) {
+  Said u;
+  u.row0 = __builtin_amdgcn_readlane(s.row0, i);
+  u.rows = __builtin_amdgcn_readlane(s.rows, i);
+  u.len = __builtin_amdgcn_readlane(s.len, i);
+  u.dead = __builtin_amdgcn_readlane(s.dead, i);
+  Req r = req_of<S>(p, u);
+  r.rounds = __builtin_amdgcn_readfirstlane(r.rounds);
+  r.col_tiles = __builtin_amdgcn_readfirstlane(r.col_tiles);
+  r.cols = __builtin_amdgcn_readfirstlane(r.cols);
   return r;
+}
+
+// a / b for a < 2^53, with the reciprocal of b
+__device__ inline uint64_t quotient(uint64_t a, uint64_t b, double reciprocal) {
+  uint64_t q = (uint64_t)((double)a * reciprocal);
+  if (q * b > a) q--;
+  if (a - q * b >= b) q++;
+  return q;
 }
 
 // Running state of one wave's 32 columns: lane l holds column l % 32; of O^T
@@ -338,23 +376,6 @@ struct State {
 #pragma unroll
     for (int t = 0; t < S::kAcc; t++) o[t] = f32x16{};
   }
-  // Adds a state with the whole sum l2 (given to one of the two lanes of a column).
-  __device__ void add(float m2, float l2, const f32x4* src, float c) {
-    const float mn = fmaxf(m, m2), safe = mn == -INFINITY ? 0.f : mn;
-    const float f1 = exp2f((m - safe) * c), f2 = exp2f((m2 - safe) * c);
-    m = mn;
-    l = l * f1 + l2 * f2;
-#pragma unroll
-    for (int t = 0; t < S::kAcc; t++)
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const f32x4 v = src[(t * 4 + q) * kWave];
-        o[t][4 * q] = o[t][4 * q] * f1 + v.x * f2;
-        o[t][4 * q + 1] = o[t][4 * q + 1] * f1 + v.y * f2;
-        o[t][4 * q + 2] = o[t][4 * q + 2] * f1 + v.z * f2;
-        o[t][4 * q + 3] = o[t][4 * q + 3] * f1 + v.w * f2;
-      }
-  }
   // dst: [kAcc * 4][64] f32x4, then [64] (m, l)
   __device__ void put(f32x4* dst, uint32_t lane) const {
 #pragma unroll
@@ -364,24 +385,10 @@ struct State {
         dst[(t * 4 + q) * kWave + lane] = f32x4{o[t][4 * q], o[t][4 * q + 1], o[t][4 * q + 2], o[t][4 * q + 3]};
     ((f32x2*)(dst + S::kAcc * 4 * kWave))[lane] = f32x2{m, l};
   }
-  // The same layout in memory that workgroups of other XCDs read: stores and loads of single words at the device's
-  // scope, past the XCDs' own L2s.  A fence would write back and drop the whole L2 instead (with one on each side,
-  // 64 requests of 128-2048 tokens took 185 us longer).
-  __device__ void publish(uint64_t* dst, uint32_t lane) const {
-#pragma unroll
-    for (int t = 0; t < S::kAcc; t++)
-#pragma unroll
-      for (int q = 0; q < 8; q++)
-        __hip_atomic_store(dst + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2,
-                           __builtin_bit_cast(uint64_t, f32x2{o[t][2 * q], o[t][2 * q + 1]}), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(dst + S::kAcc * 8 * kWave + lane, __builtin_bit_cast(uint64_t, f32x2{m, l}), __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-  }
 };
 
-__device__ inline f32x2 published(const uint8_t* part, uint32_t at) {
-  return __builtin_bit_cast(f32x2, __hip_atomic_load((const uint64_t*)part + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+__device__ inline f32x2 published(const uint64_t* at) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
 __device__ inline uint64_t uniform(uint64_t x) {
@@ -440,55 +447,76 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   }
   if (a.n_reqs == 0) return;
 
-  // this workgroup's units, and the request that holds the first of them
-  const uint32_t per = (a.n_reqs + S::kThreads - 1) / S::kThreads;
-  uint64_t mine = 0;
-  for (uint32_t i = 0; i < per; i++) {
-    const uint32_t b = tid * per + i;
-    if (b < a.n_reqs) {
-      const Req r = req_of<S>(p, b);
-      mine += (uint64_t)r.cols * r.rounds;
+  // This workgroup's units, and the request that holds the first of them.  Every workgroup sums the requests' units
+  // itself: up to 64 of them each wave for itself, a request a lane, without waiting for another; more of them the
+  // workgroup together.
+  Said said = said_of(p, lane);  // of requests b0 + lane
+  uint32_t b0 = 0, bi = 0;       // bi: the current request among them
+  uint64_t total, unit, unit_end, base;  // base: first unit of the current request
+  auto share = [&]() -> bool {
+    if (total < n_wg) {
+      if (wg >= total) return false;
+      n_wg = (uint32_t)total;  // a unit each
+    } else if (n_wg % 8 == 0) {
+      // neighbours in the order of work share an XCD (and its L2), where column tiles of one KV head read the same keys
+      wg = wg % 8 * (n_wg / 8) + wg / 8;
     }
-  }
-  uint64_t upto = mine;
+    return true;
+  };
+  auto running = [&](uint64_t v) -> uint64_t {
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const uint64_t u = __shfl_up((unsigned long long)upto, d);
-    if (lane >= (uint32_t)d) upto += u;
-  }
-  if (lane == kWave - 1) sums[wave] = upto;
-  __syncthreads();
-  uint64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < S::kWaves; w++) {
-    if ((uint32_t)w < wave) upto += sums[w];
-    total += sums[w];
-  }
-  total = uniform(total);
-  if (total < n_wg) {
-    if (wg >= total) return;
-    n_wg = (uint32_t)total;  // a unit each
-  } else if (n_wg % 8 == 0) {
-    // neighbours in the order of work share an XCD (and its L2), where column tiles of one KV head read the same keys
-    wg = wg % 8 * (n_wg / 8) + wg / 8;
-  }
-  uint64_t unit = wg * total / n_wg;
-  const uint64_t unit_end = (wg + 1ull) * total / n_wg;
-  if (upto - mine <= unit && unit < upto) {
-    uint64_t at = upto - mine;
-    uint32_t b = tid * per;
-    for (;; b++) {
-      const Req r = req_of<S>(p, b);
-      const uint64_t n = (uint64_t)r.cols * r.rounds;
-      if (unit < at + n) break;
-      at += n;
+    for (int d = 1; d < kWave; d *= 2) {
+      const uint64_t u = __shfl_up((unsigned long long)v, d);
+      if (lane >= (uint32_t)d) v += u;
     }
-    found[0] = b;
-    found[1] = at;
+    return v;
+  };
+  auto first_of = [&](uint32_t w) -> uint64_t { return quotient(w * total, n_wg, 1.0 / (double)n_wg); };
+  if (a.n_reqs <= kWave) {
+    const uint64_t mine = units_of<S>(p, said), upto = running(mine);
+    total = uniform(__shfl((unsigned long long)upto, kWave - 1));
+    if (!share()) return;
+    unit = first_of(wg);
+    bi = __builtin_ctzll(__ballot(unit < upto));
+    base = uniform(__shfl((unsigned long long)(upto - mine), bi));
+  } else {
+    const uint32_t per = (a.n_reqs + S::kThreads - 1) / S::kThreads;
+    uint64_t mine = 0;
+#pragma unroll 4
+    for (uint32_t i = 0; i < per; i++) mine += units_of<S>(p, said_of(p, tid * per + i));
+    uint64_t upto = running(mine);
+    if (lane == kWave - 1) sums[wave] = upto;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < S::kWaves; w++) {
+      if ((uint32_t)w < wave) upto += sums[w];
+      total += sums[w];
+    }
+    total = uniform(total);
+    if (!share()) return;
+    unit = first_of(wg);
+    if (upto - mine <= unit && unit < upto) {
+      uint64_t at = upto - mine;
+      uint32_t b = tid * per;
+      for (;; b++) {
+        const uint64_t n = units_of<S>(p, said_of(p, b));
+        if (unit < at + n) break;
+        at += n;
+      }
+      found[0] = b;
+      found[1] = at;
+    }
+    __syncthreads();
+    b0 = __builtin_amdgcn_readfirstlane((uint32_t)found[0]);
+    base = uniform(found[1]);
+    said = said_of(p, b0 + lane);
   }
-  __syncthreads();
-  uint32_t b = __builtin_amdgcn_readfirstlane((uint32_t)found[0]);
-  uint64_t base = uniform(found[1]);  // first unit of request b
+  // scalar from here on: divisions leave vector registers
+  unit = uniform(unit);
+  unit_end = uniform(first_of(wg + 1));
+  const uint64_t first = unit;
+  const double per_unit = 1.0 / (double)total;
 
   const float c = fmaxf(fabsf(a.scale) * 1.44269504f, 1.17549435e-38f);
   const uint32_t neg = a.scale < 0 ? 0x80008000u : 0u;
@@ -505,16 +533,22 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   uint32_t* counters = (uint32_t*)work;
   uint8_t* partials = work + 4 * kAttnCounters;
 
-  Req r = uniform_req_of<S>(p, b);
+  Req r = req_at<S>(p, said, bi);
   while (unit < unit_end) {
     while (unit >= base + (uint64_t)r.cols * r.rounds) {
       base += (uint64_t)r.cols * r.rounds;
-      r = uniform_req_of<S>(p, ++b);
+      if (++bi == kWave || !S::kKeepsRequests) {
+        b0 += bi;
+        bi = 0;
+        said = said_of(p, b0 + lane);
+      }
+      r = req_at<S>(p, said, bi);
     }
-    const uint32_t at = (uint32_t)(unit - base), column = at / r.rounds, it0 = at % r.rounds;
+    const uint32_t at = (uint32_t)(unit - base), column = __builtin_amdgcn_readfirstlane(at / r.rounds),
+                   it0 = at - column * r.rounds;
     const uint64_t col_first = unit - it0, col_last = col_first + r.rounds - 1;
     const uint32_t it1 = (uint32_t)(unit_end - unit < r.rounds - it0 ? it0 + (unit_end - unit) : r.rounds);
-    const uint32_t g = column / r.col_tiles, ct = column % r.col_tiles;
+    const uint32_t g = __builtin_amdgcn_readfirstlane(column / r.col_tiles), ct = column - g * r.col_tiles;
     // this lane's query row
     const uint32_t rows = r.rows * p.group, qrow = (ct * S::WQ + wq) * 32 + col;
     const bool qlive = qrow < rows;
@@ -539,7 +573,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
 #pragma unroll
         for (int s = 0; s < S::D / 16; s++) q[s] = __builtin_bit_cast(vec, *(const u32x4*)(qp + 32 * s) ^ neg);
       }
-      const uint32_t* tab = a.tables + b * a.table_stride;
+      const uint32_t* tab = a.tables + (uint64_t)(b0 + bi) * a.table_stride;
       const uint8_t* kbase = p.kv.base + a.layer * p.kv.layer_stride + g * p.kv.head_stride;
       const uint8_t *dk = (const uint8_t*)a.k + r.row0 * a.k_row_stride + g * a.k_head_stride,
                     *dv = (const uint8_t*)a.v + r.row0 * a.v_row_stride + g * a.v_head_stride;
@@ -781,102 +815,148 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
       st.l += other_half(st.l);
     }
 
-    // the key groups' states meet in the first group
+    // The column's states go to LDS, and from there each wave of a query group takes every WK-th 32 elements of D: the
+    // key groups' states are added on the way.  (What follows runs once a column, so it is kept short instead of
+    // unrolled: code that is not in the instruction cache yet costs more than what it does.)
     constexpr size_t kPer = S::kAcc * 4096 + 512;  // bytes of a wave's state
-    if constexpr (S::WK > 1) {
-      __syncthreads();
-      if (wk > 0) st.put((f32x4*)(area + (wave - S::WQ) * kPer), lane);
-      __syncthreads();
-      if (wk == 0) {
-#pragma unroll 1
-        for (int k = 1; k < S::WK; k++) {
-          const f32x4* src = (const f32x4*)(area + ((k - 1) * S::WQ + wq) * kPer);
-          const f32x2 ml = ((const f32x2*)(src + S::kAcc * 4 * kWave))[lane];
-          st.add(ml.x, ml.y, src + lane, c);
-        }
+    __syncthreads();
+    st.put((f32x4*)(area + wave * kPer), lane);
+    __syncthreads();
+    auto state = [&](int k) { return (const f32x4*)(area + (k * S::WQ + wq) * kPer); };
+    float m = -INFINITY, l = 0;
+    f32x2 ml[S::WK];
+#pragma unroll
+    for (int k = 0; k < S::WK; k++) {
+      ml[k] = ((const f32x2*)(state(k) + S::kAcc * 4 * kWave))[lane];
+      m = fmaxf(m, ml[k][0]);
+    }
+    {
+      const float safe = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int k = 0; k < S::WK; k++) {
+        ml[k][0] = exp2f((ml[k][0] - safe) * c);  // the state's factor
+        l += ml[k][1] * ml[k][0];
       }
     }
-    uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8;
-    auto write = [&](int t, const f32x16& o, float inv) {
+    auto chunk = [&](int t) -> f32x16 {
+      f32x16 o = f32x16{};
+#pragma unroll
+      for (int k = 0; k < S::WK; k++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          const f32x4 v = state(k)[(t * 4 + q) * kWave + lane];
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[4 * q + e] += v[e] * ml[k][0];
+        }
+      return o;
+    };
+    auto write = [&](int t, const f32x16& o, float m, float l) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8 + 64 * t;
 #pragma unroll
       for (int k = 0; k < 4; k++) {
         typedef typename E::elem elem4 __attribute__((ext_vector_type(4)));
         elem4 x;
 #pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = (typename E::elem)(o[4 * k + i] * inv);
-        *(elem4*)(op + 64 * t + 16 * k) = x;
+        for (int e = 0; e < 4; e++) x[e] = (typename E::elem)(o[4 * k + e] * inv);
+        *(elem4*)(op + 16 * k) = x;
       }
-    };
-    auto write_lse = [&](float m, float l) {
-      if (a.lse && half == 0)
+      if (a.lse && t == 0 && half == 0)
         a.lse[qtok * a.n_heads + head] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * 0.693147181f;
     };
-    const uint32_t w0 = (uint32_t)(((col_first + 1) * n_wg - 1) / total), w1 = (uint32_t)(((col_last + 1) * n_wg - 1) / total);
-    if (w0 == w1) {
-      if (wk == 0 && qlive) {
-        const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
-#pragma unroll
-        for (int t = 0; t < S::kAcc; t++) write(t, st.o[t], inv);
-        write_lse(st.m, st.l);
-      }
+    // the workgroup that has a unit: most often this one
+    auto owner = [&](uint64_t u) -> uint32_t {
+      return u >= first && u < unit_end ? wg : (uint32_t)quotient((u + 1) * n_wg - 1, total, per_unit);
+    };
+    const uint32_t w0 = owner(col_first), parts = owner(col_last) - w0 + 1;
+    if (parts == 1) {
+      if (qlive)
+#pragma unroll 1
+        for (int t = wk; t < S::kAcc; t += S::WK) write(t, chunk(t), m, l);
     } else {
-      // of a workgroup's parts at most the first joins a column begun before it, and at most the last one begins a
-      // column that others end: two places each
-      if (wk == 0 && qlive)
-        st.publish((uint64_t*)(partials + (2 * wg + (wg == w0 ? 1 : 0)) * S::kPartial + wq * kPer), lane);
-      __builtin_amdgcn_s_waitcnt(0);  // the stores have arrived before the count goes up
-      __syncthreads();
-      if (tid == 0) {
-        const uint32_t parts = w1 - w0 + 1,
-                       before = __hip_atomic_fetch_add(&counters[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last_one = before == parts - 1;
-        if (before == parts - 1)  // clear for the next call
-          __hip_atomic_store(&counters[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      __syncthreads();
-      if (last_one && qlive) {
-        // The parts' maxima and sums first, then their outputs, a group of waves every WK-th 32 elements: the loads of
-        // kAhead parts are in flight at a time.
-        constexpr uint32_t kAhead = 8;
-        auto part = [&](uint32_t w) { return partials + (2 * w + (w == w0 ? 1 : 0)) * S::kPartial + wq * kPer; };
-        float m = -INFINITY, l = 0;
-        for (uint32_t w = w0; w <= w1; w += kAhead) {
-          f32x2 ml[kAhead];
+      // A column's parts are joined by the workgroup that finishes last; many of them in two steps, by the last of each
+      // run of parts and then by the last of the runs, so that no workgroup has more than about the root of them to read
+      // (64 parts in one step: 25 us longer).
+      const uint32_t run = parts <= 8 ? parts : parts <= 64 ? 8 : parts <= 256 ? 16 : 64;
+      // Of a workgroup's parts at most the first joins a column begun before it, and at most the last one begins a
+      // column that others end: two places each.
+      auto place = [&](uint32_t w) -> uint64_t* {
+        return (uint64_t*)(partials + (2 * w + (w == w0 ? 1 : 0)) * S::kPartial + wq * (S::kPartial / S::WQ));
+      };
+      // Words that workgroups of other XCDs read: stores and loads at the device's scope, past the XCDs' own L2s.  A
+      // fence would write back and drop the whole L2 instead (64 requests of 128-2048 tokens: 185 us longer).
+      // Elements of O, then [2][64] maxima and sums: those of a part, and those of the run that begins with it.
+      auto publish = [&](uint64_t* to, int t, const f32x16& o, float m, float l, int joined) {
 #pragma unroll
-          for (uint32_t u = 0; u < kAhead; u++) ml[u] = published(part(w + u <= w1 ? w + u : w1), S::kAcc * 8 * kWave + lane);
-          float mn = m;
-#pragma unroll
-          for (uint32_t u = 0; u < kAhead; u++) mn = fmaxf(mn, ml[u][0]);
-          const float safe = mn == -INFINITY ? 0.f : mn;
-          l *= exp2f((m - safe) * c);
-          m = mn;
-#pragma unroll
-          for (uint32_t u = 0; u < kAhead; u++)
-            if (w + u <= w1) l += ml[u][1] * exp2f((ml[u][0] - safe) * c);
+        for (int q = 0; q < 8; q++)
+          __hip_atomic_store(to + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2,
+                             __builtin_bit_cast(uint64_t, f32x2{o[2 * q], o[2 * q + 1]}), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
+        if (t == 0)
+          __hip_atomic_store(to + (S::kAcc * 8 + joined) * kWave + lane, __builtin_bit_cast(uint64_t, f32x2{m, l}),
+                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      };
+      auto last_of = [&](uint32_t* counter, uint32_t n) -> bool {
+        __builtin_amdgcn_s_waitcnt(0);  // the stores have arrived before the count goes up
+        __syncthreads();
+        if (tid == 0) {
+          last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+          if (last_one) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next call
         }
-        const float safe = m == -INFINITY ? 0.f : m, inv = l == 0.f ? 0.f : 1.f / l;
-        for (uint32_t t = wk; t < (uint32_t)S::kAcc; t += S::WK) {
-          f32x16 o = f32x16{};
-          for (uint32_t w = w0; w <= w1; w += kAhead / 2) {
-            f32x2 x[kAhead / 2][8], ml[kAhead / 2];
+        __syncthreads();
+        return __builtin_amdgcn_readfirstlane(last_one);
+      };
+      if (qlive)
+#pragma unroll 1
+        for (int t = wk; t < S::kAcc; t += S::WK) publish(place(wg), t, chunk(t), m, l, 0);
+      // n published states, of every step-th workgroup from w on, in that order
+      uint32_t w = w0 + (wg - w0) / run * run, n = w0 + parts - w < run ? w0 + parts - w : run, step = 1;
+      uint32_t* counter = run == parts ? counters + w0 : counters + kAttnCounters / 4 + 2 * w + (w == w0 ? 1 : 0);
+      while (last_of(counter, n)) {
+        const bool whole = run == parts || step == run;
+        if (qlive)
+#pragma unroll 1
+          for (int t = wk; t < S::kAcc; t += S::WK) {
+            constexpr uint32_t kAhead = S::WQ == 1 && S::D <= 128 ? 8 : 4;  // states on their way at a time
+            float m = -INFINITY, l = 0;
+            f32x16 o = f32x16{};
+#pragma unroll 1
+            for (uint32_t j = 0; j < n; j += kAhead) {
+              f32x2 x[kAhead][8], ml[kAhead];
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead / 2; u++) {
-              const uint8_t* from = part(w + u <= w1 ? w + u : w1);
-              ml[u] = published(from, S::kAcc * 8 * kWave + lane);
+              for (uint32_t u = 0; u < kAhead; u++) {
+                const uint64_t* from = place(w + (j + u < n ? j + u : n - 1) * step);
+                ml[u] = published(from + (S::kAcc * 8 + (step > 1)) * kWave + lane);
 #pragma unroll
-              for (int q = 0; q < 8; q++) x[u][q] = published(from, ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2);
+                for (int q = 0; q < 8; q++) x[u][q] = published(from + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2);
+              }
+              float mn = m;
+#pragma unroll
+              for (uint32_t u = 0; u < kAhead; u++) mn = fmaxf(mn, ml[u][0]);
+              const float safe = mn == -INFINITY ? 0.f : mn, f0 = exp2f((m - safe) * c);
+              l *= f0;
+              o *= f0;
+              m = mn;
+#pragma unroll
+              for (uint32_t u = 0; u < kAhead; u++)
+                if (j + u < n) {
+                  const float f = exp2f((ml[u][0] - safe) * c);
+                  l += ml[u][1] * f;
+#pragma unroll
+                  for (int e = 0; e < 16; e++) o[e] += x[u][e / 2][e % 2] * f;
+                }
             }
-#pragma unroll
-            for (uint32_t u = 0; u < kAhead / 2; u++) {
-              if (w + u > w1) break;
-              const float f = exp2f((ml[u][0] - safe) * c);
-#pragma unroll
-              for (int i = 0; i < 16; i++) o[i] += x[u][i / 2][i % 2] * f;
-            }
+            // a run's elements take the place of its first part's, which no other wave reads
+            if (whole)
+              write(t, o, m, l);
+            else
+              publish(place(w), t, o, m, l, 1);
           }
-          write(t, o, inv);
-        }
-        if (wk == 0) write_lse(m, l);
+        if (whole) break;
+        w = w0;
+        n = (parts + run - 1) / run;
+        step = run;
+        counter = counters + w0;
       }
     }
     __syncthreads();
@@ -911,9 +991,14 @@ namespace {
 template <class E, class S, int MINW>
 hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
   // as many workgroups as run at once: MINW waves on each SIMD, four SIMDs
-  const uint32_t grid = w.cus * (4 * MINW / S::kWaves);
+  uint32_t grid = w.cus * (4 * MINW / S::kWaves);
   static_assert(4 * MINW % S::kWaves == 0, "whole workgroups");
-  if (2 * grid * S::kPartial > w.partial_bytes || grid > kAttnCounters) return hipErrorInvalidValue;
+  if (2 * grid * S::kPartial > w.partial_bytes || grid > kAttnCounters / 4) return hipErrorInvalidValue;
+  // and no more than the lengths can give work to, as far as the host knows them
+  const uint64_t tiles = (((uint64_t)a.a.table_width << a.kv.block_shift) + a.a.n_rows) / kTileKeys + 2,
+                 cols = (uint64_t)a.kv.heads * (a.a.n_rows * a.group / (32 * S::WQ) + a.a.n_reqs),
+                 rounds = tiles / S::kTiles + 1;
+  if (cols < grid && cols * rounds < grid) grid = cols * rounds ? (uint32_t)(cols * rounds) : 1;
   k_tree_attention<E, S, MINW><<<grid, S::kThreads, 0, s>>>(a, w.mem);
   return hipGetLastError();
 }

@@ -197,7 +197,7 @@ gift_status gift_attention_work_create(hipStream_t stream, gift_attention_work* 
   e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return report_hip(e, "hipDeviceGetAttribute");
   if (cus < 1) cus = 1;
-  if (cus > (int)kAttnCounters / 2) cus = kAttnCounters / 2;  // two workgroups a CU at most
+  if (cus > (int)kAttnCounters / 8) cus = kAttnCounters / 8;  // two workgroups a CU at most
   gift_attention_work w = new (std::nothrow) gift_attention_work_s{dev, {nullptr, (uint32_t)cus, 2 * kAttnPlace * cus}};
   if (!w) return report(GIFT_E_NOMEM, "host memory");
   const size_t counters = 4ull * kAttnCounters;

@@ -44,12 +44,13 @@ struct AttnArgs {
   gift_tree_attention_args a;
   uint32_t group;  // query heads of a KV head
 };
-// The attention's workspace: counters of the columns that are joined (zero
-// between calls: the workgroup that joins a column clears its counter), then
-// two places per workgroup for a column's part (at most 8 waves of 32 columns
-// of 256 elements and their maxima and sums).
+// The attention's workspace: counters of the columns that are joined and of
+// runs of their parts (zero between calls: the workgroup that counts a last
+// part clears the counter), a quarter and a half of them, then two places per
+// workgroup for a column's part.  The largest ones are those of a workgroup per
+// CU with 8 waves of 32 columns of 128 elements and their maxima and sums.
 constexpr uint32_t kAttnCounters = 16384;
-constexpr size_t kAttnPlace = 8 * (256 * 32 * 4 + 512);
+constexpr size_t kAttnPlace = 8 * (128 * 32 * 4 + 1024);
 struct AttnWork {
   uint8_t* mem;
   uint32_t cus;
