@@ -281,6 +281,7 @@ struct Shape {
   static constexpr int kLoads = kTileKeys * TK / (kRowsAtOnce * WQ);  // 16-byte loads of K (and of V) per lane and round
   static constexpr int kRows = kRowsAtOnce * kLoads;                  // rows that a wave loads in a round
   static constexpr int kAcc = D / 32;
+  static constexpr int kStepTiles = TK >= 2 ? 2 : 1;
   static constexpr bool kQueriesInLds = WQ == 1;
   // 64 requests stay in registers, four a lane; otherwise the next one is loaded when its turn comes, which shows less
   // where a column takes longer
@@ -408,7 +409,14 @@ __device__ inline const uint8_t* pointer_of(const uint8_t* p, uint32_t lane) {
   return (const uint8_t*)((uint64_t)hi << 32 | lo);
 }
 
-__device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ inline float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
+}
+__device__ inline float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // Work is cut evenly: a round (kTiles tiles of 32 keys) of a column tile (32 WQ
 // rows of one request and KV head) is a unit, and of all units in a row every
@@ -429,10 +437,16 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
                  wq = wave % S::WQ, wk = wave / S::WQ, half = lane / 32, col = lane % 32;
   uint32_t n_wg = gridDim.x, wg = blockIdx.x;
 
+  // This workgroup's units, and the request that holds the first of them.  Every workgroup sums the requests' units
+  // itself: up to 64 of them each wave for itself, a request a lane, without waiting for another; more of them the
+  // workgroup together.
+  const uint32_t row_first = a.n_reqs ? a.row_begin[0] : 0, row_last = a.n_reqs ? a.row_begin[a.n_reqs] : 0;
+  Said said{0, 0, 0, 0};  // of requests b0 + lane
+  if (a.n_reqs) said = said_of(p, lane);
   // rows of no request
   {
     const uint32_t total = (uint32_t)a.n_rows;
-    uint32_t lo = a.n_reqs ? a.row_begin[0] : 0, hi = a.n_reqs ? a.row_begin[a.n_reqs] : 0;
+    uint32_t lo = row_first, hi = row_last;
     lo = lo < total ? lo : total;
     hi = hi < lo ? lo : hi < total ? hi : total;
     const uint32_t loose = lo + (total - hi);
@@ -446,11 +460,6 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     }
   }
   if (a.n_reqs == 0) return;
-
-  // This workgroup's units, and the request that holds the first of them.  Every workgroup sums the requests' units
-  // itself: up to 64 of them each wave for itself, a request a lane, without waiting for another; more of them the
-  // workgroup together.
-  Said said = said_of(p, lane);  // of requests b0 + lane
   uint32_t b0 = 0, bi = 0;       // bi: the current request among them
   uint64_t total, unit, unit_end, base;  // base: first unit of the current request
   auto share = [&]() -> bool {
@@ -471,7 +480,9 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     }
     return v;
   };
-  auto first_of = [&](uint32_t w) -> uint64_t { return quotient(w * total, n_wg, 1.0 / (double)n_wg); };
+  auto first_of = [&](uint32_t w) -> uint64_t {
+    return n_wg == total ? w : quotient(w * total, n_wg, 1.0 / (double)n_wg);
+  };
   if (a.n_reqs <= kWave) {
     const uint64_t mine = units_of<S>(p, said), upto = running(mine);
     total = uniform(__shfl((unsigned long long)upto, kWave - 1));
@@ -516,7 +527,6 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
   unit = uniform(unit);
   unit_end = uniform(first_of(wg + 1));
   const uint64_t first = unit;
-  const double per_unit = 1.0 / (double)total;
 
   const float c = fmaxf(fabsf(a.scale) * 1.44269504f, 1.17549435e-38f);
   const uint32_t neg = a.scale < 0 ? 0x80008000u : 0u;
@@ -560,15 +570,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     if (!r.dead && r.tiles) {
       // Queries: in registers, or in LDS where all waves have the same ones and need the registers for keys on their way.
       vec q[S::kQueriesInLds ? 1 : S::D / 16];
-      if constexpr (S::kQueriesInLds) {
-        for (uint32_t u = tid; u < 32 * S::kPieces; u += S::kThreads) {
-          const uint32_t line = u / S::kPieces, row = ct * 32 + line < rows ? ct * 32 + line : 0, tok = row / p.group;
-          const uint8_t* qp = (const uint8_t*)a.q + (uint64_t)(r.row0 + tok) * a.q_row_stride +
-                              (uint64_t)(g * p.group + (row - tok * p.group)) * a.q_head_stride;
-          *(u32x4*)(queries + line * S::kKRow + u % S::kPieces * 16) = *(const u32x4*)(qp + u % S::kPieces * 16) ^ neg;
-        }
-        __syncthreads();
-      } else {
+      if constexpr (!S::kQueriesInLds) {
         const uint8_t* qp = (const uint8_t*)a.q + qtok * a.q_row_stride + head * a.q_head_stride + half * 16;
 #pragma unroll
         for (int s = 0; s < S::D / 16; s++) q[s] = __builtin_bit_cast(vec, *(const u32x4*)(qp + 32 * s) ^ neg);
@@ -660,39 +662,55 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           __syncthreads();
         }
       };
-      auto scores = [&](const uint8_t* tile) -> f32x16 {
-        f32x16 sc = f32x16{};
+      // A step takes kStepTiles tiles: two where a wave has them, whose independent products and exponentials fill each
+      // other's latencies and share one maximum.
+      constexpr int kN = S::kStepTiles;
+      auto scores = [&](const uint8_t* tile, f32x16 (&sc)[kN]) {
+#pragma unroll
+        for (int n = 0; n < kN; n++) sc[n] = f32x16{};
         const uint8_t* krow = tile + col * S::kKRow + half * 16;
 #pragma unroll
-        for (int d = 0; d < S::D / 16; d++)
-          sc = E::mfma(*(const vec*)(krow + 32 * d),
-                       S::kQueriesInLds ? *(const vec*)(queries + col * S::kKRow + half * 16 + 32 * d) : q[S::kQueriesInLds ? 0 : d], sc);
-        return sc;
+        for (int d = 0; d < S::D / 16; d++) {
+          const vec qd = S::kQueriesInLds ? *(const vec*)(queries + col * S::kKRow + half * 16 + 32 * d) : q[S::kQueriesInLds ? 0 : d];
+#pragma unroll
+          for (int n = 0; n < kN; n++) sc[n] = E::mfma(*(const vec*)(krow + n * S::kTileBytes + 32 * d), qd, sc[n]);
+        }
       };
       auto seen = [&](uint32_t see, int i) -> bool { return see >> (8 * (i / 4) + i % 4) & 1; };  // of see >> 4 half
-      // weights of a tile's keys, from their scores and flags
-      auto weigh = [&](f32x16 sc, uint32_t t, uint32_t flag, vec (&w)[2][E::kParts]) {
-        const uint32_t have = (uint32_t)__ballot(flag & 1);
-        const bool draft = t >= r.ctx_tiles;
-        uint32_t see = have;
-        if (draft) {
-          const uint32_t word = t - r.ctx_tiles;
-          if (a.mask)
-            see &= word < a.mask_words ? a.mask[qtok * a.mask_words + word] : 0u;
-          else
-            see &= token >= 32 * word + 31 ? ~0u : token < 32 * word ? 0u : (2u << (token - 32 * word)) - 1;
+      // scores of tiles t, t + 1, ... to weights; flags: row_flags of the first of them
+      auto weigh = [&](f32x16 (&sc)[kN], uint32_t t, const uint8_t (*flags)[kTileKeys]) {
+        uint32_t flag[kN], see[kN];
+        bool part = false;
+#pragma unroll
+        for (int n = 0; n < kN; n++) {
+          flag[n] = flags[n][col];
+          see[n] = (uint32_t)__ballot(flag[n] & 1);
+          part |= see[n] != ~0u;
         }
-        const bool part = draft || have != ~0u;
-        const uint32_t mine = see >> (4 * half);
+        const bool draft = t + kN > r.ctx_tiles;
+        part |= draft;
         if (part) {
 #pragma unroll
-          for (int i = 0; i < 16; i++)
-            if (!seen(mine, i)) sc[i] = -INFINITY;
-        }
-        float top = sc[0];
+          for (int n = 0; n < kN; n++) {
+            if (t + n >= r.ctx_tiles) {
+              const uint32_t word = t + n - r.ctx_tiles;
+              if (a.mask)
+                see[n] &= word < a.mask_words ? a.mask[qtok * a.mask_words + word] : 0u;
+              else
+                see[n] &= token >= 32 * word + 31 ? ~0u : token < 32 * word ? 0u : (2u << (token - 32 * word)) - 1;
+            }
+            const uint32_t mine = see[n] >> (4 * half);
 #pragma unroll
-        for (int i = 1; i < 16; i++) top = fmaxf(top, sc[i]);
-        top = fmaxf(top, other_half(top));
+            for (int i = 0; i < 16; i++)
+              if (!seen(mine, i)) sc[n][i] = -INFINITY;
+          }
+        }
+        float top = sc[0][0];
+#pragma unroll
+        for (int n = 0; n < kN; n++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) top = fmaxf(top, sc[n][i]);
+        top = max_of_halves(top);
         const float mn = fmaxf(st.m, top), safe = mn == -INFINITY ? 0.f : mn;
         if (__any(mn != st.m)) {
           const float f = exp2f((st.m - safe) * c);
@@ -702,54 +720,77 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           st.m = mn;
         }
         const float shift = -safe * c;
+        float sum[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 16; i++) sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], c, shift));
+        for (int n = 0; n < kN; n++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c, shift));
         if (part) {
 #pragma unroll
-          for (int i = 0; i < 16; i++)
-            if (!seen(mine, i)) sc[i] = 0.f;
+          for (int n = 0; n < kN; n++) {
+            const uint32_t mine = see[n] >> (4 * half);
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+              if (!seen(mine, i)) sc[n][i] = 0.f;
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 16; i++) st.l += sc[i];
-        // to the operands' type; the sum above is not rounded
-        E::parts(sc, 0, w[0]);
-        E::parts(sc, 1, w[1]);
-        uint32_t odd = draft ? (uint32_t)__ballot(flag & 2) : 0u;
-        while (odd) {  // drafted keys whose V is not finite: only for the rows that see them
-          const uint32_t key = __builtin_ctz(odd);
-          odd &= odd - 1;
-          float own = 0;
+        for (int n = 0; n < kN; n++)
 #pragma unroll
-          for (int i = 0; i < 16; i++)
-            if ((uint32_t)(8 * (i / 4) + i % 4) == (key & ~4u)) own = sc[i];
-          const float theirs = other_half(own), weight = (key >> 2 & 1) == half ? own : theirs;
-          const typename E::elem* vp =
-              (const typename E::elem*)(dv + (uint64_t)((t - r.ctx_tiles) * kTileKeys + key) * a.v_row_stride);
-          if (see >> key & 1) {
+          for (int i = 0; i < 16; i++) sum[i % 4] += sc[n][i];
+        st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (draft) {
+#pragma unroll 1
+          for (int n = 0; n < kN; n++) {
+            uint32_t odd = t + n >= r.ctx_tiles ? (uint32_t)__ballot(flag[n] & 2) : 0u;
+            while (odd) {  // drafted keys whose V is not finite: only for the rows that see them
+              const uint32_t key = __builtin_ctz(odd);
+              odd &= odd - 1;
+              float own = 0;
 #pragma unroll
-            for (int d = 0; d < S::kAcc; d++)
+              for (int i = 0; i < 16; i++)
+                if ((uint32_t)(8 * (i / 4) + i % 4) == (key & ~4u)) own = n ? sc[kN - 1][i] : sc[0][i];
+              const float theirs = other_half(own), weight = (key >> 2 & 1) == half ? own : theirs;
+              const typename E::elem* vp =
+                  (const typename E::elem*)(dv + (uint64_t)((t + n - r.ctx_tiles) * kTileKeys + key) * a.v_row_stride);
+              if ((n ? see[kN - 1] : see[0]) >> key & 1) {
 #pragma unroll
-              for (int i = 0; i < 16; i++) st.o[d][i] += weight * (float)vp[32 * d + 8 * (i / 4) + 4 * half + i % 4];
+                for (int d = 0; d < S::kAcc; d++)
+#pragma unroll
+                  for (int i = 0; i < 16; i++) st.o[d][i] += weight * (float)vp[32 * d + 8 * (i / 4) + 4 * half + i % 4];
+              }
+            }
           }
         }
       };
-      auto add_values = [&](const uint8_t* tile, const vec (&w)[2][E::kParts]) {
+      auto add_values = [&](const uint8_t* tile, const f32x16 (&p)[kN]) {
         const uint8_t* vrow = tile + kTileKeys * S::kKRow + (4 * half + lane % 16 / 4) * S::kVRow +
                               (lane / 16 % 2 * 16 + lane % 4 * 4) * 2;
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        union Frag {
+          s16x4 x[2];
+          vec v;
+        };
+        // step i: V^T of 16 keys for elements 32 d .. 32 d + 31
+        constexpr int kSteps = 2 * kN * S::kAcc;
+        auto values = [&](int i, Frag& u) {
+          const uint8_t* at = vrow + i / (2 * S::kAcc) * S::kTileBytes + i / S::kAcc % 2 * (16 * S::kVRow) + i % S::kAcc * 64;
+          u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at);
+          u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 8 * S::kVRow));
+        };
+        constexpr int kAheadV = 2;  // operands on their way while products are made
+        Frag u[kAheadV + 1];
 #pragma unroll
-        for (int d = 0; d < S::kAcc; d++)
+        for (int i = 0; i < kAheadV; i++) values(i, u[i]);
+        vec w[E::kParts];
 #pragma unroll
-          for (int k = 0; k < 2; k++) {
-            typedef __attribute__((address_space(3))) s16x4 lds4;
-            union {
-              s16x4 x[2];
-              vec v;
-            } u;
-            u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 16 * k * S::kVRow + 64 * d));
-            u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + (16 * k + 8) * S::kVRow + 64 * d));
+        for (int i = 0; i < kSteps; i++) {
+          if (i % S::kAcc == 0) E::parts(p[i / (2 * S::kAcc)], i / S::kAcc % 2, w);
+          if (i + kAheadV < kSteps) values(i + kAheadV, u[(i + kAheadV) % (kAheadV + 1)]);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < E::kParts; e++) st.o[d] = E::mfma(u.v, w[k][e], st.o[d]);
-          }
+          for (int e = 0; e < E::kParts; e++) st.o[i % S::kAcc] = E::mfma(u[i % (kAheadV + 1)].v, w[e], st.o[i % S::kAcc]);
+        }
       };
 
       if constexpr (S::WQ == 1) {
@@ -759,28 +800,49 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         u32x4 x[S::kLoads];
         const uint8_t* tile = area + wk * S::kTileBytes;
         uint32_t id = block_of(it0), next = block_of(it0 + 1);
+        constexpr int kQ = (32 * S::kPieces + S::kThreads - 1) / S::kThreads;
+        u32x4 qx[kQ];
+#pragma unroll
+        for (int i = 0; i < kQ; i++) {
+          const uint32_t u = tid + i * S::kThreads, line = u / S::kPieces,
+                         row = line < 32 && ct * 32 + line < rows ? ct * 32 + line : 0, tok = row / p.group;
+          qx[i] = *(const u32x4*)((const uint8_t*)a.q + (uint64_t)(r.row0 + tok) * a.q_row_stride +
+                                  (uint64_t)(g * p.group + (row - tok * p.group)) * a.q_head_stride + u % S::kPieces * 16);
+        }
         Row row = row_of(it0, id);
         fetch(x, row.k);
+#pragma unroll
+        for (int i = 0; i < kQ; i++) {
+          const uint32_t u = tid + i * S::kThreads;
+          if (u < 32 * S::kPieces) *(u32x4*)(queries + u / S::kPieces * S::kKRow + u % S::kPieces * 16) = qx[i] ^ neg;
+        }
         store_k(x, 0);
         fetch(x, row.v);
-        for (uint32_t it = it0; it < it1; it++) {
-          id = next;
-          next = block_of(it + 2);
+        __syncthreads();
+        for (uint32_t it = it0;; it++) {
           const uint32_t t = it * S::kTiles + wk;
-          vec w[2][E::kParts];
+          const bool more = it + 1 < it1;
+          f32x16 sc[1];
           meet();
-          const f32x16 sc = scores(tile);
+          scores(tile, sc);
           store_v(x, row, 0);
-          row = row_of(it + 1, id);
-          fetch(x, row.k);
+          if (more) {
+            id = next;
+            next = block_of(it + 2);
+            row = row_of(it + 1, id);
+            fetch(x, row.k);
+          }
           meet();
-          weigh(sc, t, row_flags[0][wk][col], w);
-          add_values(tile, w);
+          weigh(sc, t, &row_flags[0][wk]);
+          add_values(tile, sc);
+          if (!more) break;
           meet();
           store_k(x, 0);
           fetch(x, row.v);
         }
       } else {
+        // A round is in one buffer while the next one goes to the other; the one after it is on its way.  A wave that is
+        // done with its products stores and asks ahead while others still compute.
         u32x4 xk[S::kLoads], xv[S::kLoads];
         uint32_t id = block_of(it0), next = block_of(it0 + 1);
         Row row = row_of(it0, id);
@@ -800,13 +862,14 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           meet();
           if (wave_live) {
 #pragma unroll 1
-            for (int s = 0; s < S::TK; s++) {
+            for (int s = 0; s < S::TK; s += kN) {
               const uint32_t t = it * S::kTiles + wk * S::TK + s;
               if (t >= r.tiles) break;
               const uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + s) * S::kTileBytes;
-              vec w[2][E::kParts];
-              weigh(scores(tile), t, row_flags[buf][wk * S::TK + s][col], w);
-              add_values(tile, w);
+              f32x16 sc[kN];
+              scores(tile, sc);
+              weigh(sc, t, &row_flags[buf][wk * S::TK + s]);
+              add_values(tile, sc);
             }
           }
           if (it + 1 == it1) break;
@@ -866,7 +929,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     };
     // the workgroup that has a unit: most often this one
     auto owner = [&](uint64_t u) -> uint32_t {
-      return u >= first && u < unit_end ? wg : (uint32_t)quotient((u + 1) * n_wg - 1, total, per_unit);
+      if (u >= first && u < unit_end) return wg;
+      return n_wg == total ? (uint32_t)u : (uint32_t)quotient((u + 1) * n_wg - 1, total, 1.0 / (double)total);
     };
     const uint32_t w0 = owner(col_first), parts = owner(col_last) - w0 + 1;
     if (parts == 1) {
