@@ -12,6 +12,8 @@ library is not built, importing the binding's functions raises.
 """
 import ctypes
 import os
+import struct
+import sys
 
 import numpy as np
 
@@ -144,17 +146,17 @@ def lib():
         L.gift_token_encrypt.restype = st
         L.gift_token_decrypt.argtypes = [ctypes.POINTER(_SegTable), P, ctypes.c_uint64, P, ctypes.c_uint64, P, P, P]
         L.gift_token_decrypt.restype = st
-        L.gift_kv_tables.argtypes = [ctypes.POINTER(_KvStep), P]
+        L.gift_kv_tables.argtypes = [P, P]
         L.gift_kv_tables.restype = st
         L.gift_kv_append.argtypes = [ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat), P, ctypes.c_uint64, P,
-                                     ctypes.POINTER(_KvRows), P]
+                                     P, P]
         L.gift_kv_append.restype = st
         L.gift_attention_work_create.argtypes = [P, ctypes.POINTER(ctypes.c_void_p)]
         L.gift_attention_work_create.restype = st
         L.gift_attention_work_destroy.argtypes = [P]
         L.gift_attention_work_destroy.restype = st
         L.gift_tree_attention.argtypes = [P, ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat),
-                                          ctypes.POINTER(_TreeAttention), P]
+                                          P, P]
         L.gift_tree_attention.restype = st
         L.gift_profile_next_call.argtypes = [P, P]
         L.gift_profile_next_call.restype = st
@@ -234,6 +236,12 @@ def _dev(x, nbytes, name):
 
 def _stream(stream):
     if stream is None:
+        # a few microseconds less than torch.cuda.current_stream(), which builds a Stream object
+        torch = sys.modules.get("torch")
+        if torch is not None and torch.cuda.is_initialized():
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            if raw is not None:
+                return raw(torch._C._cuda_getDevice())
         try:
             import torch
             if torch.cuda.is_available():
@@ -418,9 +426,25 @@ def token_decrypt(segs, blocks, n_tokens, kt, eos_token, tokens_out, nonces_out=
 
 # --- include/gift_kv.h: the paged cache in use on the device ---
 
+def _types():
+    """Codes of the element types K and V may have, by torch's type."""
+    import torch
+    return {torch.bfloat16: BF16, torch.float16: F16}
+
+
+_codes = None
+
+
+def _code(dtype):
+    global _codes
+    if _codes is None:
+        _codes = _types()
+    return _codes.get(dtype)
+
+
 def kv_format(dtype, n_heads, head_dim, block_tokens, token_stride, head_stride, v_offset, k_offset=0):
     """gift_kv_format.  dtype: torch.bfloat16, torch.float16 or their codes (BF16, F16); offsets and strides in bytes."""
-    code = dtype if isinstance(dtype, int) else {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(dtype))
+    code = dtype if isinstance(dtype, int) else _code(dtype)
     if code is None:
         raise ValueError(f"dtype {dtype}: K and V are bfloat16 or float16")
     return _KvFormat(code, n_heads, head_dim, block_tokens, k_offset, v_offset, token_stride, head_stride)
@@ -428,8 +452,13 @@ def kv_format(dtype, n_heads, head_dim, block_tokens, token_stride, head_stride,
 
 def _ints(x, n, name, size=4):
     """Address of a device array of n integers of size bytes (a contiguous tensor of that width, or an address)."""
-    if x is not None and hasattr(x, "element_size") and x.element_size() != size:
-        raise ValueError(f"{name}: elements of {x.element_size()} bytes, the call needs {size}")
+    try:
+        if x.is_cuda and x.element_size() == size and x.numel() >= n and x.is_contiguous():
+            return x.data_ptr()
+        if x.element_size() != size:
+            raise ValueError(f"{name}: elements of {x.element_size()} bytes, the call needs {size}")
+    except AttributeError:
+        pass
     return _dev(x, size * n, name)
 
 
@@ -437,29 +466,37 @@ def _matrix(x, rows, name):
     """Address, columns and row stride (in entries) of a device [rows][columns] int32 tensor, rows any distance apart."""
     if not getattr(x, "is_cuda", False):
         raise ValueError(f"{name}: tensor must be on the GPU")
-    if x.element_size() != 4 or x.dim() != 2 or x.shape[0] < rows or (x.shape[1] > 1 and x.stride(1) != 1):
+    shape = x.shape
+    if x.element_size() != 4 or len(shape) != 2 or shape[0] < rows or (shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{name}: needs {rows} rows of adjacent 32-bit entries")
-    return x.data_ptr(), x.shape[1], max(x.stride(0), x.shape[1]) if x.shape[0] < 2 else x.stride(0)
+    return x.data_ptr(), shape[1], max(x.stride(0), shape[1]) if shape[0] < 2 else x.stride(0)
 
 
-def _rows_of(x, fmt, lead, heads, name):
-    """Address and byte strides of a device tensor [*lead][heads][head_dim] of the format's type, whose last dimension
-    is contiguous; dimensions of one element have stride 0."""
+def _rows_of(x, fmt, want, name):
+    """Address and byte strides of a device tensor of shape want, (..., heads, head_dim), of the format's type, whose last
+    dimension is contiguous; dimensions of one element have stride 0."""
     if not getattr(x, "is_cuda", False):
         raise ValueError(f"{name}: tensor must be on the GPU")
-    if {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(x.dtype)) != fmt.dtype:
+    if _code(x.dtype) != fmt.dtype:
         raise ValueError(f"{name}: {x.dtype} is not the cache's type")
-    want = (*lead, heads, fmt.head_dim)
-    if tuple(x.shape) != want:
+    if x.shape != want:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {want}")
-    if x.stride(-1) != 1:
+    strides = x.stride()
+    if strides[-1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return x.data_ptr(), [0 if x.shape[d] <= 1 else 2 * x.stride(d) for d in range(len(want) - 1)]
+    return x.data_ptr(), [2 * s if n > 1 else 0 for n, s in zip(want, strides[:-1])]
 
 
 def _same_format(kv, fmt):
     if not isinstance(kv, _PagedKV) or not isinstance(fmt, _KvFormat):
         raise TypeError("kv and fmt come from paged_kv() and kv_format()")
+
+
+# the argument structures as packed bytes: filling a ctypes structure takes several times as long
+_STEP = struct.Struct("@IIQPPPPIIQPPPQPPPP")
+_ROWS = struct.Struct("@PPQ6Q")
+_TREE = struct.Struct("@QIIIfPPPPP8QPPPIQPIP")
+assert (_STEP.size, _ROWS.size, _TREE.size) == tuple(map(ctypes.sizeof, (_KvStep, _KvRows, _TreeAttention)))
 
 
 def kv_tables(users, lens, new_lens, block_tokens, free_blocks, tables, block_labels, slots, row_begin, lens_out, taken,
@@ -469,12 +506,12 @@ def kv_tables(users, lens, new_lens, block_tokens, free_blocks, tables, block_la
     taken int32 [1]."""
     n = users.numel()
     tab, width, stride = _matrix(tables, n, "tables")
-    s = _KvStep(n, block_tokens, block_labels.numel(), _ints(users, n, "users"), _ints(lens, n, "lens"),
-                _ints(new_lens, n, "new_lens"), _ints(free_blocks, 0, "free_blocks"), free_blocks.numel(), width, stride,
-                tab, _ints(block_labels, 1, "block_labels"), _ints(slots, 0, "slots", 8), slots.numel(),
-                _ints(row_begin, n + 1, "row_begin"), _ints(lens_out, n, "lens_out"), _ints(taken, 1, "taken"),
-                _ints(verdicts, n, "verdicts"))
-    _check(lib().gift_kv_tables(ctypes.byref(s), _stream(stream)))
+    s = _STEP.pack(n, block_tokens, block_labels.numel(), _ints(users, n, "users"), _ints(lens, n, "lens"),
+                   _ints(new_lens, n, "new_lens"), _ints(free_blocks, 0, "free_blocks"), free_blocks.numel(), width,
+                   stride, tab, _ints(block_labels, 1, "block_labels"), _ints(slots, 0, "slots", 8), slots.numel(),
+                   _ints(row_begin, n + 1, "row_begin"), _ints(lens_out, n, "lens_out"), _ints(taken, 1, "taken"),
+                   _ints(verdicts, n, "verdicts"))
+    _check(lib().gift_kv_tables(s, _stream(stream)))
 
 
 def kv_append(kv, fmt, slots, k, v, index=None, stream=None):
@@ -482,14 +519,15 @@ def kv_append(kv, fmt, slots, k, v, index=None, stream=None):
     [n_layers][n_rows][heads][head_dim], any strides but the last; index device int32 [n_slots] or None."""
     _same_format(kv, fmt)
     n = slots.numel()
-    rows = k.shape[1] if k.dim() == 4 else 0
-    kp, ks = _rows_of(k, fmt, (kv.n_layers, rows), fmt.n_heads, "k")
-    vp, vs = _rows_of(v, fmt, (kv.n_layers, rows), fmt.n_heads, "v")
-    r = _KvRows(kp, vp, rows, *ks, *vs)
+    rows = k.shape[1] if len(k.shape) == 4 else 0
+    want = (kv.n_layers, rows, fmt.n_heads, fmt.head_dim)
+    kp, ks = _rows_of(k, fmt, want, "k")
+    vp, vs = _rows_of(v, fmt, want, "v")
     if index is None and rows < n:
         raise ValueError(f"k: {rows} rows, the call needs {n}")
-    _check(lib().gift_kv_append(ctypes.byref(kv), ctypes.byref(fmt), _ints(slots, n, "slots", 8), n,
-                                _ints(index, n, "index"), ctypes.byref(r), _stream(stream)))
+    _check(lib().gift_kv_append(kv, fmt, _ints(slots, n, "slots", 8), n,
+                                None if index is None else _ints(index, n, "index"), _ROWS.pack(kp, vp, rows, *ks, *vs),
+                                _stream(stream)))
 
 
 class AttentionWork:
@@ -518,23 +556,29 @@ def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, 
     both None; any strides but the last.  row_begin int32 [n_reqs + 1]; lens, verdicts int32 [n_reqs]; tables int32
     [n_reqs][width]; mask int32 [n_rows][words]; lse float32 [n_rows][n_heads].  scale defaults to head_dim ** -0.5."""
     _same_format(kv, fmt)
-    n, (rows, heads) = lens.numel(), (q.shape[0], q.shape[1] if q.dim() == 3 else 0)
-    qp, qs = _rows_of(q, fmt, (rows,), heads, "q")
-    op, os_ = _rows_of(out, fmt, (rows,), heads, "out")
-    (kp, ks), (vp, vs) = (_rows_of(x, fmt, (rows,), fmt.n_heads, name) if x is not None else (None, [0, 0])
-                          for x, name in ((k, "k"), (v, "v")))
+    n, shape = lens.numel(), q.shape
+    rows, heads = (shape[0], shape[1]) if len(shape) == 3 else (0, 0)
+    dim = fmt.head_dim
+    qp, qs = _rows_of(q, fmt, (rows, heads, dim), "q")
+    op, os_ = _rows_of(out, fmt, (rows, heads, dim), "out")
+    kp = vp = 0
+    ks = vs = (0, 0)
+    if k is not None:
+        kp, ks = _rows_of(k, fmt, (rows, fmt.n_heads, dim), "k")
+    if v is not None:
+        vp, vs = _rows_of(v, fmt, (rows, fmt.n_heads, dim), "v")
     tab, width, stride = _matrix(tables, n, "tables")
-    words = 0
+    words = mp = 0
     if mask is not None:
-        if mask.dim() != 2 or mask.shape[0] < rows:
+        if len(mask.shape) != 2 or mask.shape[0] < rows:
             raise ValueError(f"mask: needs {rows} rows of words")
         words = mask.shape[1]
-    a = _TreeAttention(rows, n, heads, layer, fmt.head_dim ** -0.5 if scale is None else scale, qp, kp, vp, op,
-                       _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_, _ints(row_begin, n + 1, "row_begin"),
-                       _ints(lens, n, "lens"), tab, width, stride, _ints(mask, rows * words, "mask"), words,
-                       _ints(verdicts, n, "verdicts"))
-    _check(lib().gift_tree_attention(work.handle, ctypes.byref(kv), ctypes.byref(fmt), ctypes.byref(a),
-                                     _stream(stream)))
+        mp = _ints(mask, rows * words, "mask")
+    a = _TREE.pack(rows, n, heads, layer, dim ** -0.5 if scale is None else scale, qp, kp, vp, op,
+                   0 if lse is None else _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_,
+                   _ints(row_begin, n + 1, "row_begin"), _ints(lens, n, "lens"), tab, width, stride, mp, words,
+                   0 if verdicts is None else _ints(verdicts, n, "verdicts"))
+    _check(lib().gift_tree_attention(work.handle, kv, fmt, a, _stream(stream)))
 
 
 def profile_next_call(before, after):

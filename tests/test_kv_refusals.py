@@ -17,7 +17,8 @@ def lib():
     if not os.path.exists(gift.LIB_PATH):
         from paper_2608_25431_amd import build
         build.build()
-    return gift.lib()
+    yield gift.lib()
+    gift.lib().gift_attention_work_destroy(None)  # leaves no message behind for other tests
 
 
 def cache(**over):
@@ -173,8 +174,8 @@ class Fake:
     def element_size(self):
         return self.size
 
-    def stride(self, d):
-        return self.strides[d]
+    def stride(self, d=None):
+        return tuple(self.strides) if d is None else self.strides[d]
 
     def is_contiguous(self):
         return True
