@@ -218,6 +218,11 @@ def _dev(x, nbytes, name):
     contiguous CUDA tensor that large (a host buffer, or one too short, would
     make the kernels fault instead of failing here); an int is taken as a
     device address as is; None is NULL."""
+    try:
+        if x.is_cuda and x.is_contiguous() and x.nbytes >= nbytes:
+            return x.data_ptr()
+    except AttributeError:
+        pass  # no tensor, or one to be looked at more closely below
     if x is None or isinstance(x, int):
         return x
     if isinstance(x, np.ndarray):
@@ -484,7 +489,8 @@ def _rows_of(x, fmt, want, name):
     strides = x.stride()
     if strides[-1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return x.data_ptr(), [2 * s if n > 1 else 0 for n, s in zip(want, strides[:-1])]
+    return x.data_ptr(), [2 * s for s in strides[:-1]] if min(want) > 1 else \
+        [2 * s if n > 1 else 0 for n, s in zip(want, strides[:-1])]
 
 
 def _same_format(kv, fmt):
