@@ -715,13 +715,12 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         }
       };
       auto seen = [&](uint32_t see, int i) -> bool { return see >> (8 * (i / 4) + i % 4) & 1; };  // of see >> 4 half
-      // scores of tiles t, t + 1, ... to weights; flags: row_flags of the first of them
-      auto weigh = [&](f32x16 (&sc)[kN], uint32_t t, const uint8_t (*flags)[kTileKeys]) {
-        uint32_t flag[kN], see[kN];
+      // scores of tiles t, t + 1, ... to weights; flag: their row_flags of row `col`
+      auto weigh = [&](f32x16 (&sc)[kN], uint32_t t, const uint32_t (&flag)[kN]) {
+        uint32_t see[kN];
         bool part = false;
 #pragma unroll
         for (int n = 0; n < kN; n++) {
-          flag[n] = flags[n][col];
           see[n] = (uint32_t)__ballot(flag[n] & 1);
           part |= see[n] != ~0u;
         }
@@ -763,15 +762,6 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         for (int n = 0; n < kN; n++)
 #pragma unroll
           for (int i = 0; i < 16; i++) sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c, shift));
-        if (part) {
-#pragma unroll
-          for (int n = 0; n < kN; n++) {
-            const uint32_t mine = see[n] >> (4 * half);
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-              if (!seen(mine, i)) sc[n][i] = 0.f;
-          }
-        }
 #pragma unroll
         for (int n = 0; n < kN; n++)
 #pragma unroll
@@ -871,7 +861,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
             fetch(x, row.k);
           }
           meet();
-          weigh(sc, t, &row_flags[0][wk]);
+          const uint32_t flag[1] = {row_flags[0][wk][col]};
+          weigh(sc, t, flag);
           add_values(tile, sc);
           if (!more) break;
           meet();
@@ -905,8 +896,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
               if (t >= r.tiles) break;
               const uint8_t* tile = area + (buf * S::kTiles + wk * S::TK + s) * S::kTileBytes;
               f32x16 sc[kN];
+              uint32_t flag[kN];
+#pragma unroll
+              for (int n = 0; n < kN; n++) flag[n] = row_flags[buf][wk * S::TK + s + n][col];
               scores(tile, sc);
-              weigh(sc, t, &row_flags[buf][wk * S::TK + s]);
+              weigh(sc, t, flag);
               add_values(tile, sc);
             }
           }
@@ -1105,20 +1099,24 @@ hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Waves that share a tile of keys, by the rows that a request has on average
-// at a KV head.
+// Waves that share a tile of keys, by the rows that a request has on average at
+// a KV head.  Two workgroups of four waves a CU run out of step with each
+// other, one's products under the other's barrier; from 129 rows on eight waves
+// share a tile, so that keys are not read twice.  In us, 64 requests of 128-2048
+// tokens with 8 / 16 / 32 drafted tokens at a group of 4 (32, 64, 128 rows): a
+// wave each 91 / 137 / 282; two 112 / 89 / 228; four 115 / 114 / 143; eight
+// 129 / 127 / 163.  32 requests of 2048-8192 tokens, 192 rows: four 358, eight 312.
+// With 256 elements a wave takes all registers of its SIMD, and four waves are
+// as many as there are.
 template <class E, int D>
 hipError_t attend_by_rows(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
   const uint64_t rows = a.a.n_reqs ? (a.a.n_rows * a.group + a.a.n_reqs - 1) / a.a.n_reqs : 1;
-  if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, D <= 128 ? 2 : 1>(a, w, s);
-  if constexpr (D <= 128) {
-    if (rows <= 64) return attend<E, Shape<D, 2, 4, 1>, 2>(a, w, s);
-    if (rows <= 128) return attend<E, Shape<D, 4, 2, 2>, 2>(a, w, s);
-    return attend<E, Shape<D, 8, 1, 4>, 2>(a, w, s);
-  } else {
-    if (rows <= 64) return attend<E, Shape<D, 2, 2, 1>, 1>(a, w, s);
-    return attend<E, Shape<D, 4, 1, 2>, 1>(a, w, s);
-  }
+  constexpr int kPerSimd = D <= 128 ? 2 : 1;
+  if (rows <= 32) return attend<E, Shape<D, 1, 4, 1>, kPerSimd>(a, w, s);
+  if (rows <= 64) return attend<E, Shape<D, 2, 2, 1>, kPerSimd>(a, w, s);
+  if constexpr (D <= 128)
+    if (rows > 128) return attend<E, Shape<D, 8, 1, 4>, kPerSimd>(a, w, s);
+  return attend<E, Shape<D, 4, 1, 2>, kPerSimd>(a, w, s);
 }
 
 template <class E>
