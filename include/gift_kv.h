@@ -141,7 +141,7 @@ typedef struct {
 gift_status gift_kv_append(const gift_paged_kv* kv, const gift_kv_format* format, const int64_t* slots,
                            uint64_t n_slots, const uint32_t* index, const gift_kv_rows* rows, hipStream_t stream);
 
-/* Device workspace of gift_tree_attention (about 68 MB): calls that are
+/* Device workspace of gift_tree_attention (about 72 MB): calls that are
  * ordered on one stream, and graphs replayed there, may share one; calls that
  * may overlap need one each. */
 typedef struct gift_attention_work_s* gift_attention_work;

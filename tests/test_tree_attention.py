@@ -16,6 +16,15 @@ def work():
     return gift.AttentionWork()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("drafts", [[3, 9, 1], [14, 10, 3], [33, 20, 15], [70, 31, 49]])
+def test_rows_that_share_keys(work, dim, dtype, drafts):
+    # 17, 36, 90 and 200 rows at a KV head on average: each number of waves that share a tile, with part-filled ones
+    b = Batch([201, 0, 1030], drafts, dtype, heads=2, group=4, dim=dim, mask="holes", seed=dim + drafts[0])
+    b.check(b.run(work))
+
+
 LENS = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 257, 400]
 
 
@@ -41,7 +50,8 @@ def test_heads_and_layouts(work, heads, group, drafts, block, order, parts):
 
 @pytest.mark.parametrize("lens,drafts,heads,group,dim", [
     ([5000], [3], 2, 4, 128), ([9001, 1], [1, 1], 1, 1, 64), ([3000, 0, 1700], [20, 6, 1], 1, 8, 96),
-    ([4100], [40], 1, 4, 256), ([2500, 2499], [50, 60], 1, 2, 128)])
+    ([4100], [40], 1, 4, 256), ([2500, 2499], [50, 60], 1, 2, 128),
+    ([20001, 5], [3, 1], 1, 2, 64), ([40000], [2], 1, 1, 96)])  # parts joined in runs of 16 and of 64
 def test_long_axes_are_split_and_joined(work, lens, drafts, heads, group, dim):
     b = Batch(lens, drafts, "f16" if dim == 64 else "bf16", heads=heads, group=group, dim=dim, seed=7, q_scale=2.0)
     got = b.run(work)
