@@ -90,10 +90,10 @@ typedef struct {
  *   Blocks: requests take blocks from the front of the free list in request
  *     order, as many as their new tokens need beyond their last block.  The
  *     blocks are entered in the request's table row and labelled with its
- *     user.  A request whose tokens would pass table_width takes none; from
- *     the first request on that the free list cannot serve whole, no request
- *     that needs a block gets one.  taken[0] is the number of blocks that
- *     left the list.
+ *     user.  A request whose tokens would pass table_width takes none, nor do
+ *     requests whose rows pass n_slots; from the first request on that the
+ *     free list cannot serve whole, no request that needs a block gets one.
+ *     taken[0] is the number of blocks that left the list.
  *   Slots: slots[row] = block * block_tokens + place of the token, where the
  *     row's K and V belong in the cache; -1 for rows of a request whose
  *     verdict is not OK and for rows of no request.

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
       const Sums upto = carry + scan<T>(own, lds, &all);
       if (b < n) {
         a.s.row_begin[b + 1] = (uint32_t)(upto.rows < a.s.n_slots ? upto.rows : a.s.n_slots);
-        if (need && upto.blocks <= a.s.n_free) taken = upto.blocks;
+        if (need && upto.blocks <= a.s.n_free && upto.rows <= a.s.n_slots) taken = upto.blocks;
       }
       carry = carry + all;
     }
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
       const Ask o = ask_of(a, p);
       before = before + Sums{o.need, o.add};
     }
-    granted = k.fits && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
+    granted = k.fits && before.rows + k.add <= a.s.n_slots && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
     from = a.s.free_blocks + before.blocks;  // read only where granted
     if (granted)
       for (uint32_t j = lane; j < k.need; j += TPR) bad |= from[j] >= a.s.n_blocks ? 2u : 0u;
@@ -164,8 +164,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
   if (b >= n) return;
   bad = flags[group];
   granted = granted && !(bad & 2u);
-  const bool room = before.rows + k.add <= a.s.n_slots;
-  const int32_t verdict = (bad & 1u) ? GIFT_SEG_OWNER_MIXED : (granted && room) ? GIFT_SEG_OK : GIFT_SEG_NO_SPACE;
+  const int32_t verdict = (bad & 1u) ? GIFT_SEG_OWNER_MIXED : granted ? GIFT_SEG_OK : GIFT_SEG_NO_SPACE;
   if (granted)
     for (uint32_t j = lane; j < k.need; j += TPR) {
       const uint32_t id = from[j];

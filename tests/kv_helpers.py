@@ -197,7 +197,7 @@ def expect_tables(users, lens, new, block, free, tab, labels, n_slots):
         fits = want <= width
         need = want - have if fits else 0
         upto += need
-        got = fits and (need == 0 or upto <= len(free))
+        got = fits and row + add <= n_slots and (need == 0 or upto <= len(free))
         if got and need:
             taken = upto
         ids = [int(x) for x in free[upto - need:upto]] if got else []
@@ -207,8 +207,7 @@ def expect_tables(users, lens, new, block, free, tab, labels, n_slots):
         for j, i in enumerate(ids):
             tab[b, have + j] = i
             labels[i] = users[b]
-        ok = got and row + add <= n_slots
-        verdicts.append(gift.SEG_OWNER_MIXED if mixed else gift.SEG_OK if ok else gift.SEG_NO_SPACE)
+        verdicts.append(gift.SEG_OWNER_MIXED if mixed else gift.SEG_OK if got else gift.SEG_NO_SPACE)
         if verdicts[-1] == gift.SEG_OK:
             for i in range(add):
                 slots[row + i] = tab[b, (length + i) // block] * block + (length + i) % block

@@ -129,3 +129,14 @@ def test_no_requests():
     gift.kv_tables(empty, empty, empty, 16, empty, torch.zeros(0, 4, dtype=torch.int32, device=DEV), i32([0, 1]), slots,
                    first, empty, taken, empty)
     assert slots.tolist() == [-1] * 5 and first.item() == 0 and taken.item() == 0
+
+
+def test_requests_without_slots_take_no_blocks():
+    # the last two requests' rows pass the slot array: their blocks stay in the free list for a later step
+    c = make(np.random.default_rng(10), 6, 16, 0, 50, 20, 40, 3)
+    c["n_slots"] = int(c["new"][:4].sum()) + 1
+    want = check(c)
+    before = c["tab"]
+    assert (want["tables"][4:] == before[4:]).all() and (want["tables"][:4] != before[:4]).any()
+    assert want["taken"][0] == (-(-(c["lens"] + c["new"]) // 16) - -(-c["lens"] // 16))[:4].sum()
+    assert (want["verdicts"] == [gift.SEG_OK] * 4 + [gift.SEG_NO_SPACE] * 2).all()
