@@ -418,10 +418,15 @@ __device__ inline uint32_t fresh(uint32_t x) {
   return x;
 }
 
-__device__ inline const uint8_t* pointer_of(const uint8_t* p, uint32_t lane) {
+// Global memory by name: a pointer put together from integers would load by flat instructions, which count among the LDS
+// accesses too, so that every wait for LDS would wait for the rows on their way.
+typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
+typedef const __attribute__((address_space(1))) u32x4* global_pieces;
+
+__device__ inline global_bytes pointer_of(const uint8_t* p, uint32_t lane) {
   const uint32_t lo = __builtin_amdgcn_ds_bpermute(4 * lane, (uint32_t)(uintptr_t)p),
                  hi = __builtin_amdgcn_ds_bpermute(4 * lane, (uint32_t)((uintptr_t)p >> 32));
-  return (const uint8_t*)((uint64_t)hi << 32 | lo);
+  return (global_bytes)((uint64_t)hi << 32 | lo);
 }
 
 __device__ inline float other_half(float x) {
@@ -639,8 +644,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         const uint32_t first = fresh(at_once);
 #pragma unroll
         for (int i = 0; i < S::kLoads; i++) {
-          const uint8_t* from = pointer_of(rows, i * S::kRowsAtOnce + first);
-          x[i] = *(const u32x4*)(from + read_at);
+          const global_bytes from = pointer_of(rows, i * S::kRowsAtOnce + first);
+          x[i] = *(global_pieces)(from + read_at);
         }
       };
       // Fourth step: into LDS.
