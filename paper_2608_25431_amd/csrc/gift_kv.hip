@@ -711,11 +711,22 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
 #pragma unroll
         for (int n = 0; n < kN; n++) sc[n] = f32x16{};
         const uint8_t* krow = tile + col * S::kKRow + half * 16;
+        constexpr int kSteps = S::D / 16, kAheadK = 2;  // operands on their way while products are made
+        vec kd[kAheadK + 1][kN], qd[kAheadK + 1];
+        auto keys = [&](int d) {
 #pragma unroll
-        for (int d = 0; d < S::D / 16; d++) {
-          const vec qd = S::kQueriesInLds ? *(const vec*)(queries + col * S::kKRow + half * 16 + 32 * d) : q[S::kQueriesInLds ? 0 : d];
+          for (int n = 0; n < kN; n++) kd[d % (kAheadK + 1)][n] = *(const vec*)(krow + n * S::kTileBytes + 32 * d);
+          qd[d % (kAheadK + 1)] = S::kQueriesInLds ? *(const vec*)(queries + col * S::kKRow + half * 16 + 32 * d)
+                                                   : q[S::kQueriesInLds ? 0 : d];
+        };
 #pragma unroll
-          for (int n = 0; n < kN; n++) sc[n] = E::mfma(*(const vec*)(krow + n * S::kTileBytes + 32 * d), qd, sc[n]);
+        for (int d = 0; d < kAheadK; d++) keys(d);
+#pragma unroll
+        for (int d = 0; d < kSteps; d++) {
+          if (d + kAheadK < kSteps) keys(d + kAheadK);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int n = 0; n < kN; n++) sc[n] = E::mfma(kd[d % (kAheadK + 1)][n], qd[d % (kAheadK + 1)], sc[n]);
         }
       };
       auto seen = [&](uint32_t see, int i) -> bool { return see >> (8 * (i / 4) + i % 4) & 1; };  // of see >> 4 half
