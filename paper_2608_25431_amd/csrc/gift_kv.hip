@@ -384,7 +384,7 @@ __device__ inline uint64_t quotient(uint64_t a, uint64_t b, double reciprocal) {
 // the elements d = 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
 template <class S>
 struct State {
-  float m, l;  // maximum (unscaled score), this lane's part of the sum
+  float m, l;  // what the weights refer to (an unscaled score), this lane's part of the sum
   f32x16 o[S::kAcc];
   __device__ void clear() {
     m = -INFINITY;
@@ -763,8 +763,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
 #pragma unroll
           for (int i = 0; i < 16; i++) top = fmaxf(top, sc[n][i]);
         top = max_of_halves(top);
-        const float mn = fmaxf(st.m, top), safe = mn == -INFINITY ? 0.f : mn;
-        if (__any(mn != st.m)) {
+        // What weights refer to need not be the maximum itself: while no score passes it by 8 octaves it stays, and the
+        // sums with it (random scores raise the maximum of some column in most steps).
+        const bool grow = __any((top - st.m) * c > 8.f);
+        const float mn = grow ? fmaxf(st.m, top) : st.m, safe = mn == -INFINITY ? 0.f : mn;
+        if (grow) {
           const float f = exp2f((st.m - safe) * c);
           st.l *= f;
 #pragma unroll
@@ -914,9 +917,14 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
               uint32_t flag[kN];
 #pragma unroll
               for (int n = 0; n < kN; n++) flag[n] = row_flags[buf][wk * S::TK + s + n][col];
+              // a wave's products go before another's exponentials on the SIMD (32 requests of 2048-8192 tokens: 306 -> 302)
+              __builtin_amdgcn_s_setprio(1);
               scores(tile, sc);
+              __builtin_amdgcn_s_setprio(0);
               weigh(sc, t, flag);
+              __builtin_amdgcn_s_setprio(1);
               add_values(tile, sc);
+              __builtin_amdgcn_s_setprio(0);
             }
           }
           if (it + 1 == it1) break;

@@ -259,3 +259,12 @@ def test_a_captured_step_replays(work):
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
         assert torch.equal(b.cache.data.view(torch.int16), want[2].view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("q_scale", [0.3, 3.0, 12.0])
+@pytest.mark.parametrize("drafts", [[4, 3], [40, 45]])
+def test_scores_that_stay_and_that_jump(work, dtype, q_scale, drafts):
+    # maxima that later keys pass by less than the weights' reference follows, and by far more
+    b = Batch([1500, 333], drafts, dtype, heads=1, group=4, dim=128, seed=24, q_scale=q_scale)
+    b.check(b.run(work))
