@@ -196,9 +196,10 @@ typedef struct {
  * not seen.  lens past table_width * block_tokens are cut to it; row_begin is
  * taken as rising and cut to n_rows.
  * Scores, maxima, sums and the running output are 32-bit floats; for the
- * product with V the weights exp(s_j - m), with m at most 5.6 below the
- * largest score, are rounded to 16 significant bits (bfloat16, in two parts)
- * or to 11 (float16), and the output is rounded once at the end.  The same inputs give the same bits.
+ * product with V the weights exp(s_j - m) are rounded to 16 significant bits
+ * (bfloat16, in two parts; m at most 5.6 below the largest score) or to 11
+ * (float16; m the largest score), and the output is rounded once at the end.
+ * The same inputs give the same bits.
  *   out must not overlap q, k, v or the cache.
  * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, head counts,
  * layer, scale, the format), GIFT_E_RANGE (chunks exceed cache_bytes),

@@ -70,10 +70,12 @@ __device__ Sums scan(Sums v, Sums* lds, Sums* all) {
 
 // TPR threads serve a request, T make a workgroup.  Which blocks a request
 // takes and where its rows start are running sums over the requests before
-// it; every workgroup sums those itself (12 B of L2-resident lengths per
-// request), so that one launch suffices.  Workgroup 0 writes what belongs to
-// no single request: the row ranges, the count of taken blocks and the slots
-// past the last row.
+// it; every workgroup sums those itself (8 B of L2-resident lengths per
+// request), so that one launch suffices.  Bound by latency: lengths, ids, labels
+// and slots wait for each other (1024 requests of 128-2048 tokens 5.4 us, 32 of
+// up to 131072 tokens 9.0 us, of which a launch that does nothing is about 4).
+// Workgroup 0 writes what belongs to no single request: the row ranges, the
+// count of taken blocks and the slots past the last row.
 template <int TPR, int T>
 __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
   __shared__ Sums lds[T / kWave];
@@ -245,6 +247,7 @@ struct Bf16 {
   // Weights are 8 bits of bfloat16 in two operands, the upper half of the float and what is left of it: with one
   // operand their rounding would add as much error again as the output's own.
   static constexpr int kParts = 2;
+  static constexpr float kSlack = 8.f;  // octaves that a score may pass what the weights refer to
   __device__ static void parts(const f32x16& p, int k, vec* w) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -259,8 +262,10 @@ struct F16 {
   typedef f16x8 vec;
   typedef _Float16 elem;
   static constexpr uint16_t kExp = 0x7C00;
-  // one operand: 11 bits of weights against 11 of the output
+  // One operand: 11 bits of weights against 11 of the output.  They refer to the maximum itself, whose own weight is then
+  // 1 and is not rounded (8 octaves of slack: errors of 131072 tokens 17% larger, and no faster).
   static constexpr int kParts = 1;
+  static constexpr float kSlack = 0.f;
   __device__ static void parts(const f32x16& p, int k, vec* w) {
 #pragma unroll
     for (int i = 0; i < 8; i++) w[0][i] = (elem)p[8 * k + i];
@@ -443,6 +448,13 @@ __device__ inline float max_of_halves(float x) {
 // workgroup takes the same number, whichever requests they belong to.  A column
 // whose units lie in several workgroups is joined by the one that finishes last,
 // in the order of the parts, so that the result does not depend on who that is.
+// Bound by memory where rows are few: K and V of 131072 tokens (8 heads of 128
+// elements, 537 MB) take 111 us, 4.8 TB/s, which is what a large copy reaches.
+// With many rows by what a wave does one after the other: 32 requests of
+// 2048-8192 tokens with trees of 16-32 tokens and 64 heads (729 MB, 142 GFLOP)
+// take 286 us.  Without products and exponentials the loads and stores alone take
+// 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
+// two waves a SIMD that meet once a round hide a third of that.
 template <class E, class S, int MINW>
 __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p, uint8_t* work) {
   typedef typename E::vec vec;
@@ -763,9 +775,9 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
 #pragma unroll
           for (int i = 0; i < 16; i++) top = fmaxf(top, sc[n][i]);
         top = max_of_halves(top);
-        // What weights refer to need not be the maximum itself: while no score passes it by 8 octaves it stays, and the
-        // sums with it (random scores raise the maximum of some column in most steps).
-        const bool grow = __any((top - st.m) * c > 8.f);
+        // What weights refer to need not be the maximum itself: while no score passes it by kSlack octaves it stays, and
+        // the sums with it (random scores raise the maximum of some column in most steps).
+        const bool grow = __any((top - st.m) * c > E::kSlack);
         const float mn = grow ? fmaxf(st.m, top) : st.m, safe = mn == -INFINITY ? 0.f : mn;
         if (grow) {
           const float f = exp2f((st.m - safe) * c);
@@ -1125,10 +1137,12 @@ hipError_t attend(const AttnArgs& a, const AttnWork& w, hipStream_t s) {
 // Waves that share a tile of keys, by the rows that a request has on average at
 // a KV head.  Two workgroups of four waves a CU run out of step with each
 // other, one's products under the other's barrier; from 129 rows on eight waves
-// share a tile, so that keys are not read twice.  In us, 64 requests of 128-2048
-// tokens with 8 / 16 / 32 drafted tokens at a group of 4 (32, 64, 128 rows): a
-// wave each 91 / 137 / 282; two 112 / 89 / 228; four 115 / 114 / 143; eight
-// 129 / 127 / 163.  32 requests of 2048-8192 tokens, 192 rows: four 358, eight 312.
+// share a tile, so that keys are not read twice.  In us, the same inputs call
+// after call, 64 requests of 128-2048 tokens with 1 / 8 / 16 / 24 / 32 drafted
+// tokens at a group of 4 (4, 32, 64, 96, 128 rows): a wave each 58 / 68 / 99 /
+// 147 / 206; two 66 / 74 / 79 / 119 / 158; four 76 / 83 / 84 / 107 / 133; eight
+// 111 / 107 / 116 / 111 / 154.  32 requests of 2048-8192 tokens, 192 rows on
+// average: one 783, two 443, four 347, eight 286.
 // With 256 elements a wave takes all registers of its SIMD, and four waves are
 // as many as there are.
 template <class E, int D>
