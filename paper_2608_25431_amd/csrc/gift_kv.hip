@@ -776,10 +776,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           for (int i = 0; i < 16; i++) top = fmaxf(top, sc[n][i]);
         top = max_of_halves(top);
         // What weights refer to need not be the maximum itself: while no score passes it by kSlack octaves it stays, and
-        // the sums with it (random scores raise the maximum of some column in most steps).
-        const bool grow = __any((top - st.m) * c > E::kSlack);
-        const float mn = grow ? fmaxf(st.m, top) : st.m, safe = mn == -INFINITY ? 0.f : mn;
-        if (grow) {
+        // the sums with it (random scores raise the maximum of some column in most steps).  A column's own scores decide,
+        // so that a row's bits do not depend on the rows beside it.
+        const bool grow = (top - st.m) * c > E::kSlack;
+        const float mn = grow ? top : st.m, safe = mn == -INFINITY ? 0.f : mn;
+        if (__any(grow)) {
           const float f = exp2f((st.m - safe) * c);
           st.l *= f;
 #pragma unroll

@@ -268,3 +268,15 @@ def test_scores_that_stay_and_that_jump(work, dtype, q_scale, drafts):
     # maxima that later keys pass by less than the weights' reference follows, and by far more
     b = Batch([1500, 333], drafts, dtype, heads=1, group=4, dim=128, seed=24, q_scale=q_scale)
     b.check(b.run(work))
+
+
+@pytest.mark.parametrize("drafts", [7, 25, 60])
+def test_rows_do_not_depend_on_the_rows_beside_them(work, drafts):
+    # other queries in the same call, some far larger: a row that does not see their keys has the same bits
+    b = Batch([900], [drafts], heads=1, group=4, dim=128, seed=25)
+    b.bits = np.eye(drafts, b.bits.shape[1], dtype=np.uint8)
+    one = b.run(work)
+    b.qkv[1:, :4] *= 9.0
+    two = b.run(work)
+    assert torch.equal(one[0][0], two[0][0]) and torch.equal(one[1][0], two[1][0])
+    assert not torch.equal(one[0][1:], two[0][1:])
