@@ -218,13 +218,13 @@ def _dev(x, nbytes, name):
     contiguous CUDA tensor that large (a host buffer, or one too short, would
     make the kernels fault instead of failing here); an int is taken as a
     device address as is; None is NULL."""
+    if x is None or isinstance(x, int):
+        return x
     try:
         if x.is_cuda and x.is_contiguous() and x.nbytes >= nbytes:
             return x.data_ptr()
     except AttributeError:
         pass  # no tensor, or one to be looked at more closely below
-    if x is None or isinstance(x, int):
-        return x
     if isinstance(x, np.ndarray):
         raise ValueError(f"{name}: a numpy array is host memory; pass a CUDA tensor or a device address")
     if hasattr(x, "data_ptr"):
