@@ -633,16 +633,18 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
       struct Row {
         const uint8_t *k, *v;
         bool ok;       // it exists
-        bool drafted;  // the round's rows of this wave may hold drafted keys
+        bool drafted;  // it is past the cached keys
+        bool any;      // the round's rows of this wave may hold drafted keys
       };
       auto row_of = [&](uint32_t it, uint32_t id) -> Row {
         const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
         Row x;
-        x.drafted = (it * S::kTiles + wk * S::TK + S::TK) * kTileKeys > ctx_keys;
+        x.any = (it * S::kTiles + wk * S::TK + S::TK) * kTileKeys > ctx_keys;
+        x.drafted = x.any && j >= ctx_keys;
         x.k = kbase + id * p.kv.block_stride + (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride;
         x.v = x.k + p.kv.v_off;
         x.ok = it < it1 && j < r.len && id < p.kv.n_blocks;
-        if (x.drafted && j >= ctx_keys) {
+        if (x.drafted) {
           const uint32_t t = j - ctx_keys;
           x.ok = it < it1 && a.k && t < r.rows;
           x.k = dk + t * a.k_row_stride;
@@ -670,7 +672,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
             *(u32x4*)(at + i * kStep / kTileKeys * S::kTileBytes + i * kStep % kTileKeys * S::kKRow) = x[i];
       };
       // V rows of keys that do not exist, and drafted ones that are not finite, are stored as zeros: a weight of zero
-      // times NaN would reach every row.
+      // times NaN would reach every row.  Cached ones stay as they are, since every row of the request sees them.
       auto store_v = [&](u32x4 (&x)[S::kLoads], const Row& row, uint32_t buf) {
         uint32_t flag = row.ok ? 1u : 0u;
         const uint64_t oks = __ballot(row.ok);
@@ -680,7 +682,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           for (int i = 0; i < S::kLoads; i++)
             if (!(mine >> (i * S::kRowsAtOnce) & 1)) x[i] = u32x4{0, 0, 0, 0};
         }
-        if (row.drafted) {
+        if (row.any) {
+          const uint32_t mine = (uint32_t)(__ballot(row.drafted) >> fresh(at_once));
           u16x2 top[S::kLoads], all{0, 0};  // largest exponents of a piece's elements
 #pragma unroll
           for (int i = 0; i < S::kLoads; i++) {
@@ -688,6 +691,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
 #pragma unroll
             for (int e = 0; e < 4; e++)
               top[i] = __builtin_elementwise_max(top[i], __builtin_bit_cast(u16x2, x[i][e] & (E::kExp * 0x10001u)));
+            if (!(mine >> (i * S::kRowsAtOnce) & 1)) top[i] = u16x2{0, 0};
             all = __builtin_elementwise_max(all, top[i]);
           }
           if (__any(all[0] == E::kExp || all[1] == E::kExp)) {
