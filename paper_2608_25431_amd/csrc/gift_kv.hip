@@ -275,6 +275,11 @@ struct F16 {
 
 constexpr int kTileKeys = 32;
 
+// Weights are exp2(c s - c m) by one multiplication and addition, with c m rounded once: off by up to half its last place,
+// the same factor for every key until the reference m moves.  From 4096 on (a factor of 1 +- 2^-13) what the rounding left
+// out is subtracted; without it, weights of scores past 2^31 would all be 0 or infinite.
+constexpr float kFarShift = 4096.f;
+
 // WQ waves share a tile of keys, each with 32 columns of its own; WK groups of
 // them take different keys, TK tiles a group in a round.
 template <int D_, int WQ_, int WK_, int TK_>
@@ -792,11 +797,20 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           st.m = mn;
         }
         const float shift = -safe * c;
+        if (__any(fabsf(shift) > kFarShift)) {
+          // what the product's rounding left out, for the columns whose own scores need it
+          const float left = fabsf(shift) > kFarShift ? __builtin_fmaf(safe, c, shift) : 0.f;
+#pragma unroll
+          for (int n = 0; n < kN; n++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c, shift) - left);
+        } else {
+#pragma unroll
+          for (int n = 0; n < kN; n++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c, shift));
+        }
         float sum[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int n = 0; n < kN; n++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c, shift));
 #pragma unroll
         for (int n = 0; n < kN; n++)
 #pragma unroll
