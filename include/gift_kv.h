@@ -198,7 +198,8 @@ typedef struct {
  * Scores, maxima, sums and the running output are 32-bit floats; for the
  * product with V the weights exp(s_j - m) are rounded to 16 significant bits
  * (bfloat16, in two parts; m at most 5.6 below the largest score) or to 11
- * (float16; m the largest score), and the output is rounded once at the end.
+ * (float16; m the largest score so far; weights under 2^-29 of the largest to
+ * steps of 2^-39 of it), and the output is rounded once at the end.
  * The same inputs give the same bits.
  *   out must not overlap q, k, v or the cache.
  * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, head counts,

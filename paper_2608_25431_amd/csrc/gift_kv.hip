@@ -248,6 +248,7 @@ struct Bf16 {
   // operand their rounding would add as much error again as the output's own.
   static constexpr int kParts = 2;
   static constexpr float kSlack = 8.f;  // octaves that a score may pass what the weights refer to
+  static constexpr float kTop = 0.f;    // octaves by which all weights are raised
   __device__ static void parts(const f32x16& p, int k, vec* w) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -263,9 +264,12 @@ struct F16 {
   typedef _Float16 elem;
   static constexpr uint16_t kExp = 0x7C00;
   // One operand: 11 bits of weights against 11 of the output.  They refer to the maximum itself, whose own weight is then
-  // 1 and is not rounded (8 octaves of slack: errors of 131072 tokens 17% larger, and no faster).
+  // not rounded (8 octaves of slack: errors of 131072 tokens 17% larger, and no faster).  That weight is 2^15, so that the
+  // type's range below it is used: 11 bits down to 2^-29 of the maximum's, steps of 2^-39 of it below.  With the maximum's
+  // at 1 there would be steps of 2^-24 from 2^-14 on and nothing below 2^-25, while the sum holds weights in 32 bits: beside
+  // a key of large score whose V is near 0, the others would lose their part in the output.
   static constexpr int kParts = 1;
-  static constexpr float kSlack = 0.f;
+  static constexpr float kSlack = 0.f, kTop = 15.f;
   __device__ static void parts(const f32x16& p, int k, vec* w) {
 #pragma unroll
     for (int i = 0; i < 8; i++) w[0][i] = (elem)p[8 * k + i];
@@ -394,7 +398,7 @@ __device__ inline uint64_t quotient(uint64_t a, uint64_t b, double reciprocal) {
 // the elements d = 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
 template <class S>
 struct State {
-  float m, l;  // what the weights refer to (an unscaled score), this lane's part of the sum
+  float m, l;  // what the weights refer to (an unscaled score), this lane's part of the sum of weights
   f32x16 o[S::kAcc];
   __device__ void clear() {
     m = -INFINITY;
@@ -796,10 +800,12 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
           for (int d = 0; d < S::kAcc; d++) st.o[d] *= f;
           st.m = mn;
         }
-        const float shift = -safe * c;
-        if (__any(fabsf(shift) > kFarShift)) {
+        float shift = -safe * c;
+        const bool far = fabsf(shift) > kFarShift;
+        if (E::kTop != 0.f && !far) shift += E::kTop;
+        if (__any(far)) {
           // what the product's rounding left out, for the columns whose own scores need it
-          const float left = fabsf(shift) > kFarShift ? __builtin_fmaf(safe, c, shift) : 0.f;
+          const float left = far ? __builtin_fmaf(safe, c, shift) - E::kTop : 0.f;
 #pragma unroll
           for (int n = 0; n < kN; n++)
 #pragma unroll
@@ -1001,6 +1007,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
     };
     auto write = [&](int t, const f32x16& o, float m, float l) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
+      constexpr float kUnit = 1.f / (float)(1u << (int)E::kTop);
       uint8_t* op = (uint8_t*)a.out + qtok * a.out_row_stride + head * a.out_head_stride + half * 8 + 64 * t;
 #pragma unroll
       for (int k = 0; k < 4; k++) {
@@ -1011,7 +1018,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
         *(elem4*)(op + 16 * k) = x;
       }
       if (a.lse && t == 0 && half == 0)
-        a.lse[qtok * a.n_heads + head] = l == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * 0.693147181f;
+        a.lse[qtok * a.n_heads + head] = l == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l * kUnit)) * 0.693147181f;
     };
     // the workgroup that has a unit: most often this one
     auto owner = [&](uint64_t u) -> uint32_t {
