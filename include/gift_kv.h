@@ -100,12 +100,20 @@ typedef struct {
  *   Verdicts: OWNER_MIXED if one of the blocks that already held tokens is
  *     labelled otherwise than the request's user or lies outside the cache;
  *     else NO_SPACE if the request's tokens do not fit or the free list gives
- *     it an id outside the cache; else OK.  Which blocks a request takes goes
+ *     it an id outside the cache or a block with another owner's label (a
+ *     released block's label is set back to GIFT_LABEL_UNOWNED before its id
+ *     is listed again); else OK.  Which blocks a request takes goes
  *     by the lengths alone: the blocks of a request that turns out mixed are
  *     entered and labelled all the same, so that they are released with it.
+ *     Of a request that the list gives a wrong id no block is entered or
+ *     labelled.
  *   lens_out[b] = lens[b] + new_lens[b] for OK requests, else lens[b].
- * The ids of the free list are distinct and no table names them; otherwise
- * labels and verdicts of the requests concerned are those of one of them.
+ * The ids of the free list are distinct and no table names them.  If they are
+ * not, still no block comes to two users and none changes its owner: of the
+ * users that the list gives the same id one at most gets it (which one, if
+ * any, may differ from call to call), and a request whose table names a block
+ * that another user's request takes is OWNER_MIXED.  Requests of one user may
+ * then share a block.
  * Outputs must not overlap inputs (GIFT_E_INVALID), except that tables and
  * block_labels are both.
  * Errors: GIFT_E_INVALID (null arrays, block_tokens no power of two, n_reqs

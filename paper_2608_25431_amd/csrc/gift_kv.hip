@@ -35,6 +35,18 @@ __device__ inline Ask ask_of(const TablesArgs& a, uint32_t b) {
   return k;
 }
 
+// The label that block id had.
+__device__ inline uint32_t claim(const TablesArgs& a, uint32_t id, uint32_t user) {
+  uint32_t label = GIFT_LABEL_UNOWNED;
+  __hip_atomic_compare_exchange_strong(a.s.block_labels + id, &label, user, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return label;
+}
+
+__device__ inline void disown(const TablesArgs& a, uint32_t id) {
+  __hip_atomic_store(a.s.block_labels + id, GIFT_LABEL_UNOWNED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 struct Sums {
   uint64_t blocks, rows;
 };
@@ -72,8 +84,9 @@ __device__ Sums scan(Sums v, Sums* lds, Sums* all) {
 // takes and where its rows start are running sums over the requests before
 // it; every workgroup sums those itself (8 B of L2-resident lengths per
 // request), so that one launch suffices.  Bound by latency: lengths, ids, labels
-// and slots wait for each other (1024 requests of 128-2048 tokens 5.4 us, 32 of
-// up to 131072 tokens 9.0 us, of which a launch that does nothing is about 4).
+// and slots wait for each other (1024 requests of 128-2048 tokens 6.1 us, 32 of
+// up to 131072 tokens 9.7 us, of which a launch that does nothing is about 4;
+// about 0.6 us of it is the claim of new blocks).
 // Workgroup 0 writes what belongs to no single request: the row ranges, the
 // count of taken blocks and the slots past the last row.
 template <int TPR, int T>
@@ -150,6 +163,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
   }
   scan<T>(mine, lds, &before);
   bool granted = false;
+  uint32_t claimed = lane;  // this thread has claimed blocks lane, lane + TPR, ... below this one
   const uint32_t* from = nullptr;
   if (b < n) {
     for (uint32_t p = first; p < b; p++) {
@@ -158,21 +172,47 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
     }
     granted = k.fits && before.rows + k.add <= a.s.n_slots && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
     from = a.s.free_blocks + before.blocks;  // read only where granted
+    // A block is claimed by swapping its label from unowned to the user, so that no two users get it and none gets what
+    // another owns, whatever the free list holds; four in flight per thread.  One that has the user's label already may
+    // be taken (a step may be run again) but is not given back with the others if the request is refused: the slots of
+    // the request's rows, at least one a block and each written by one thread, hold which is which until they are known.
     if (granted)
-      for (uint32_t j = lane; j < k.need; j += TPR) bad |= from[j] >= a.s.n_blocks ? 2u : 0u;
+      for (; claimed < k.need; claimed += 4 * TPR) {
+        uint32_t id[4], label[4];
+        bool all = true;
+#pragma unroll
+        for (int u = 0; u < 4; u++) id[u] = claimed + u * TPR < k.need ? from[claimed + u * TPR] : 0;
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          label[u] = user;  // as it was found
+          if (claimed + u * TPR < k.need) label[u] = id[u] < a.s.n_blocks ? claim(a, id[u], user) : GIFT_LABEL_PARAM;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++) all = all && (label[u] == GIFT_LABEL_UNOWNED || label[u] == user);
+        if (!all) {
+#pragma unroll
+          for (int u = 0; u < 4; u++)
+            if (label[u] == GIFT_LABEL_UNOWNED) disown(a, id[u]);
+          bad |= 2u;
+          break;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+          if (claimed + u * TPR < k.need) a.s.slots[before.rows + claimed + u * TPR] = label[u] == GIFT_LABEL_UNOWNED;
+      }
     if (bad) atomicOr(&flags[group], bad);
   }
   __syncthreads();
   if (b >= n) return;
   bad = flags[group];
-  granted = granted && !(bad & 2u);
+  if (granted && (bad & 2u)) {
+    granted = false;
+    for (uint32_t j = lane; j < k.need && j < claimed; j += TPR)
+      if (a.s.slots[before.rows + j]) disown(a, from[j]);
+  }
   const int32_t verdict = (bad & 1u) ? GIFT_SEG_OWNER_MIXED : granted ? GIFT_SEG_OK : GIFT_SEG_NO_SPACE;
   if (granted)
-    for (uint32_t j = lane; j < k.need; j += TPR) {
-      const uint32_t id = from[j];
-      row[k.have + j] = id;
-      a.s.block_labels[id] = user;
-    }
+    for (uint32_t j = lane; j < k.need; j += TPR) row[k.have + j] = from[j];
   if (lane == 0) {
     a.s.verdicts[b] = verdict;
     a.s.lens_out[b] = verdict == GIFT_SEG_OK ? k.len + k.add : k.len;
