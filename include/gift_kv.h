@@ -98,7 +98,9 @@ typedef struct {
  *     row's K and V belong in the cache; -1 for rows of a request whose
  *     verdict is not OK and for rows of no request.
  *   Verdicts: OWNER_MIXED if one of the blocks that already held tokens is
- *     labelled otherwise than the request's user or lies outside the cache;
+ *     labelled otherwise than the request's user or lies outside the cache,
+ *     or if its user is one of the labels that no user has
+ *     (GIFT_LABEL_PARAM, GIFT_LABEL_UNOWNED; it takes no blocks then);
  *     else NO_SPACE if the request's tokens do not fit or the free list gives
  *     it an id outside the cache or a block with another owner's label (a
  *     released block's label is set back to GIFT_LABEL_UNOWNED before its id

@@ -145,6 +145,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
   if (b < n) {
     k = ask_of(a, b);
     user = a.s.users[b];
+    if (user >= GIFT_LABEL_PARAM) bad = 1;  // no user: what these labels stand for is nobody's
     row = a.s.tables + (uint64_t)b * a.s.table_stride;
     // owner check of the blocks that hold tokens, eight in flight per thread
     const uint32_t have = k.have < a.s.table_width ? k.have : a.s.table_width;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
       const Ask o = ask_of(a, p);
       before = before + Sums{o.need, o.add};
     }
-    granted = k.fits && before.rows + k.add <= a.s.n_slots && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
+    granted = user < GIFT_LABEL_PARAM && k.fits && before.rows + k.add <= a.s.n_slots && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
     from = a.s.free_blocks + before.blocks;  // read only where granted
     // A block is claimed by swapping its label from unowned to the user, so that no two users get it and none gets what
     // another owns, whatever the free list holds; four in flight per thread.  One that has the user's label already may

@@ -125,3 +125,20 @@ def test_tables_that_name_free_blocks(n, hi):
         # the first and the last requests may have taken such a block themselves; the others named somebody else's
         assert (got["verdicts"][3:n - 3:3] == gift.SEG_OWNER_MIXED).all()
         assert (np.delete(got["verdicts"], np.arange(0, n, 3)) == gift.SEG_OK).all()
+
+
+@pytest.mark.parametrize("n,nhi", [(20, 60), (5, 9000)])
+def test_labels_that_no_user_has(n, nhi):
+    # blocks of the model's parameters, or nobody's, are not a request's because it says so
+    r = np.random.default_rng(n)
+    c = users_of_their_own(make(r, n, 16, 30, 300, nhi // 2, nhi, 1))
+    for b, label in ((1, gift.LABEL_UNOWNED), (3, gift.LABEL_PARAM)):
+        c["users"][b] = label
+        c["labels"][c["tab"][b, :-(-c["lens"][b] // 16)]] = label
+    got = run(c)
+    conserved(c, got)
+    assert got["verdicts"].tolist() == [gift.SEG_OWNER_MIXED if b in (1, 3) else gift.SEG_OK for b in range(n)]
+    rows = got["row_begin"]
+    for b in (1, 3):
+        assert (got["tables"][b] == c["tab"][b].astype(np.uint32).view(np.int32)).all()
+        assert (got["slots"][rows[b]:rows[b + 1]] == -1).all() and got["lens_out"][b] == c["lens"][b]
