@@ -91,7 +91,7 @@ typedef struct {
  *     order, as many as their new tokens need beyond their last block.  The
  *     blocks are entered in the request's table row and labelled with its
  *     user.  A request whose tokens would pass table_width takes none, nor do
- *     requests whose rows pass n_slots; from the first request on that the
+ *     requests with rows that pass n_slots; from the first request on that the
  *     free list cannot serve whole, no request that needs a block gets one.
  *     taken[0] is the number of blocks that left the list.
  *   Slots: slots[row] = block * block_tokens + place of the token, where the

@@ -171,7 +171,8 @@ __global__ __launch_bounds__(T) void k_kv_tables(TablesArgs a) {
       const Ask o = ask_of(a, p);
       before = before + Sums{o.need, o.add};
     }
-    granted = user < GIFT_LABEL_PARAM && k.fits && before.rows + k.add <= a.s.n_slots && (k.need == 0 || before.blocks + k.need <= a.s.n_free);
+    granted = user < GIFT_LABEL_PARAM && k.fits && (k.add == 0 || before.rows + k.add <= a.s.n_slots) &&
+              (k.need == 0 || before.blocks + k.need <= a.s.n_free);
     from = a.s.free_blocks + before.blocks;  // read only where granted
     // A block is claimed by swapping its label from unowned to the user, so that no two users get it and none gets what
     // another owns, whatever the free list holds; four in flight per thread.  One that has the user's label already may
