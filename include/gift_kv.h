@@ -109,6 +109,13 @@ typedef struct {
  *     entered and labelled all the same, so that they are released with it.
  *     Of a request that the list gives a wrong id no block is entered or
  *     labelled.
+ *   Release: where entries past a request's blocks hold an id outside the
+ *     cache, its row names, whatever the verdict, the blocks that it holds,
+ *     those taken in this step among them.  A mixed request keeps its length,
+ *     so that a further step with new tokens would take blocks again and enter
+ *     them over these: it is released first, or adds nothing.  Ids among the
+ *     first taken[0] whose label is GIFT_LABEL_UNOWNED afterwards came to
+ *     nobody and may be listed again.
  *   lens_out[b] = lens[b] + new_lens[b] for OK requests, else lens[b].
  * The ids of the free list are distinct and no table names them.  If they are
  * not, still no block comes to two users and none changes its owner: of the
