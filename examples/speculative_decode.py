@@ -9,8 +9,10 @@ The model is a small decoder with random weights.  What the framework does here:
            gift.kv_append     their K and V, all layers, into the cache
            gift.seal_paged    each request under its user's key
   handoff  gift.open_paged    into other blocks of the decode worker's cache
-  a step   gift.tree_attention  the drafted tree of every request over its cached tokens, layer by layer
-           gift.kv_tables     blocks and slots for what was accepted, and the owner check of what was there
+  a step   gift.kv_tables     the owner check of the blocks that the step will read, nothing added yet
+           gift.tree_attention  the drafted tree of every request over its cached tokens, layer by layer, under the
+                              check's verdicts
+           gift.kv_tables     blocks and slots for what was accepted, and the owner check once more
            gift.kv_append     the accepted rows, all layers
   at last  gift.seal_paged    the requests' blocks, to be swapped out
 
@@ -134,7 +136,9 @@ def tree_of(root, likely, width, depth):
 
 
 def step(model, worker, work, trees, lens):
-    """Logits of every tree's nodes, and K and V of all layers."""
+    """Logits of every tree's nodes, and K and V of all layers.  A request whose table names another user's block reads
+    none of it: its attention is zeros."""
+    _, verdicts = worker.grow([0] * len(trees))
     counts = [len(t) for t, _ in trees]
     begin = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
     mask, places = np.zeros((sum(counts), -(-max(counts) // 32) * 32), np.uint8), []
@@ -155,7 +159,8 @@ def step(model, worker, work, trees, lens):
     for layer in range(LAYERS):
         q, k, v = (t.to(torch.bfloat16) for t in model.project(x, layer))
         out = torch.empty_like(q)
-        gift.tree_attention(work, worker.kv, worker.fmt, layer, q, k, v, begin, worker.lens, worker.tables, out, mask=mask)
+        gift.tree_attention(work, worker.kv, worker.fmt, layer, q, k, v, begin, worker.lens, worker.tables, out, mask=mask,
+                            verdicts=verdicts)
         keys.append(k)
         values.append(v)
         x = x + out.float().reshape(-1, HIDDEN) @ model.out[layer]
