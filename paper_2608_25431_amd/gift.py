@@ -579,6 +579,8 @@ def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, 
         if len(mask.shape) != 2 or mask.shape[0] < rows:
             raise ValueError(f"mask: needs {rows} rows of words")
         words = mask.shape[1]
+        if rows and words == 0:  # its address would be NULL, which stands for no mask
+            raise ValueError("mask: needs at least one word a row")
         mp = _ints(mask, rows * words, "mask")
     a = _TREE.pack(rows, n, heads, layer, dim ** -0.5 if scale is None else scale, qp, kp, vp, op,
                    0 if lse is None else _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_,

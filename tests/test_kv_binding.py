@@ -1,0 +1,53 @@
+"""What the binding of the paged-cache calls checks before it calls the library, without a GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_25431_amd import gift  # noqa: E402
+from test_kv_refusals import Fake, cache, form  # noqa: E402
+
+I = torch.int32
+
+
+class Recorder:
+    """Stands in for the library: takes every call and remembers its arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return gift.OK
+        return call
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(gift, "lib", lambda: r)
+    return r
+
+
+def attend(work=None, stream=0, **over):
+    a = dict(q=Fake((6, 32, 128)), k=Fake((6, 8, 128)), v=Fake((6, 8, 128)), row_begin=Fake((3,), I), lens=Fake((2,), I),
+             tables=Fake((2, 4), I), out=Fake((6, 32, 128)), mask=Fake((6, 1), I), verdicts=Fake((2,), I),
+             lse=Fake((6, 32), torch.float32))
+    a.update(over)
+    work = work or type("W", (), {"handle": None})
+    gift.tree_attention(work, cache(), form(), 0, a["q"], a["k"], a["v"], a["row_begin"], a["lens"], a["tables"], a["out"],
+                        mask=a["mask"], verdicts=a["verdicts"], lse=a["lse"], stream=stream)
+
+
+class Empty(Fake):
+    def data_ptr(self):
+        return 0 if self.numel() == 0 else Fake.data_ptr(self)
+
+
+def test_a_mask_of_no_words_is_not_no_mask(recorder):
+    attend()
+    with pytest.raises(ValueError, match="mask: needs at least one word"):
+        attend(mask=Empty((6, 0), I))
+    none = dict(q=Empty((0, 32, 128)), out=Empty((0, 32, 128)), k=Empty((0, 8, 128)), v=Empty((0, 8, 128)))
+    attend(mask=Empty((0, 0), I), lse=None, **none)
+    assert [name for name, _ in recorder.calls] == ["gift_tree_attention"] * 2
