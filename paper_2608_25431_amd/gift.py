@@ -536,18 +536,38 @@ def kv_append(kv, fmt, slots, k, v, index=None, stream=None):
                                 _stream(stream)))
 
 
+def _work_create(stream):
+    h = ctypes.c_void_p()
+    _check(lib().gift_attention_work_create(stream, ctypes.byref(h)))
+    return h.value
+
+
 class AttentionWork:
-    """Owns a gift_attention_work handle: one for each stream that calls tree_attention."""
+    """Owns the workspaces (gift_attention_work) of tree_attention: one for the stream that it is made on, and another for
+    each further stream that calls with it, made at the first call there (which allocates 72 MB and waits for that
+    stream), so that calls on several streams may overlap.  Calls that are being captured use the first one: replay such
+    graphs on the stream that the object was made on, or in order with its calls there."""
 
     def __init__(self, stream=None):
-        h = ctypes.c_void_p()
-        _check(lib().gift_attention_work_create(_stream(stream), ctypes.byref(h)))
-        self.handle = h.value
+        self.stream = _stream(stream) or 0
+        self.others = {}  # by stream
+        self.handle = _work_create(self.stream)
+
+    def on(self, stream):
+        """The workspace for calls on another stream than the first."""
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            return self.handle
+        h = self.others.get(stream)
+        if h is None:
+            h = self.others[stream] = _work_create(stream)
+        return h
 
     def destroy(self):
         if self.handle:
-            h, self.handle = self.handle, None
-            _check(lib().gift_attention_work_destroy(h))
+            hs, self.handle, self.others = [self.handle, *self.others.values()], None, {}
+            for s in [lib().gift_attention_work_destroy(h) for h in hs]:
+                _check(s)
 
     def __del__(self):
         try:
@@ -586,7 +606,10 @@ def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, 
                    0 if lse is None else _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_,
                    _ints(row_begin, n + 1, "row_begin"), _ints(lens, n, "lens"), tab, width, stride, mp, words,
                    0 if verdicts is None else _ints(verdicts, n, "verdicts"))
-    _check(lib().gift_tree_attention(work.handle, kv, fmt, a, _stream(stream)))
+    stream, handle = _stream(stream) or 0, work.handle
+    if handle and stream != work.stream:
+        handle = work.on(stream)
+    _check(lib().gift_tree_attention(handle, kv, fmt, a, stream))
 
 
 def profile_next_call(before, after):

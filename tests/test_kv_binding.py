@@ -10,16 +10,25 @@ I = torch.int32
 
 
 class Recorder:
-    """Stands in for the library: takes every call and remembers its arguments."""
+    """Stands in for the library: takes every call and remembers its arguments; workspaces are numbers from 100 on."""
 
     def __init__(self):
-        self.calls = []
+        self.calls, self.made = [], 100
 
     def __getattr__(self, name):
         def call(*args):
             self.calls.append((name, args))
             return gift.OK
         return call
+
+    def gift_attention_work_create(self, stream, out):
+        self.calls.append(("gift_attention_work_create", (stream,)))
+        out._obj.value = self.made
+        self.made += 1
+        return gift.OK
+
+    def of(self, name, at=0):
+        return [args[at] for n, args in self.calls if n == name]
 
 
 @pytest.fixture
@@ -51,3 +60,21 @@ def test_a_mask_of_no_words_is_not_no_mask(recorder):
     none = dict(q=Empty((0, 32, 128)), out=Empty((0, 32, 128)), k=Empty((0, 8, 128)), v=Empty((0, 8, 128)))
     attend(mask=Empty((0, 0), I), lse=None, **none)
     assert [name for name, _ in recorder.calls] == ["gift_tree_attention"] * 2
+
+
+def test_calls_on_several_streams_have_a_workspace_each(recorder, monkeypatch):
+    capturing = [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    work = gift.AttentionWork(stream=7)
+    for stream in (7, 9, 0, 9, 7, 0):
+        attend(work, stream)
+    capturing[0] = True  # nothing may be made now: captured calls use the first one
+    attend(work, 9)
+    attend(work, 5)
+    used = recorder.of("gift_tree_attention")
+    assert used == [100, 101, 102, 101, 100, 102, 100, 100]
+    assert recorder.of("gift_attention_work_create") == [7, 9, 0]
+    assert recorder.of("gift_tree_attention", 4) == [7, 9, 0, 9, 7, 0, 9, 5]
+    work.destroy()
+    work.destroy()
+    assert sorted(recorder.of("gift_attention_work_destroy")) == [100, 101, 102]
