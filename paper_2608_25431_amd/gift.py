@@ -536,6 +536,14 @@ def kv_append(kv, fmt, slots, k, v, index=None, stream=None):
                                 _stream(stream)))
 
 
+_dropped = []  # workspaces whose objects went without destroy(): freed when the next one is made or destroyed
+
+
+def _free_dropped():
+    while _dropped:
+        _check(lib().gift_attention_work_destroy(_dropped.pop()))
+
+
 def _work_create(stream):
     h = ctypes.c_void_p()
     _check(lib().gift_attention_work_create(stream, ctypes.byref(h)))
@@ -552,6 +560,7 @@ class AttentionWork:
         self.stream = _stream(stream) or 0
         self.others = {}  # by stream
         self.handle = _work_create(self.stream)
+        _free_dropped()
 
     def on(self, stream):
         """The workspace for calls on another stream than the first."""
@@ -563,15 +572,20 @@ class AttentionWork:
             h = self.others[stream] = _work_create(stream)
         return h
 
-    def destroy(self):
+    def _let_go(self):
         if self.handle:
-            hs, self.handle, self.others = [self.handle, *self.others.values()], None, {}
-            for s in [lib().gift_attention_work_destroy(h) for h in hs]:
-                _check(s)
+            _dropped.extend([self.handle, *self.others.values()])
+            self.handle, self.others = None, {}
+
+    def destroy(self):
+        """Frees the workspaces; synchronises the device first."""
+        self._let_go()
+        _free_dropped()
 
     def __del__(self):
+        # May run at any time, also while a graph is captured, which a synchronisation would break.
         try:
-            self.destroy()
+            self._let_go()
         except Exception:
             pass
 

@@ -27,6 +27,9 @@ class Recorder:
         self.made += 1
         return gift.OK
 
+    def gift_last_error(self):
+        return b"no memory"
+
     def of(self, name, at=0):
         return [args[at] for n, args in self.calls if n == name]
 
@@ -78,3 +81,22 @@ def test_calls_on_several_streams_have_a_workspace_each(recorder, monkeypatch):
     work.destroy()
     work.destroy()
     assert sorted(recorder.of("gift_attention_work_destroy")) == [100, 101, 102]
+
+
+def test_a_dropped_workspace_is_freed_later(recorder):
+    work = gift.AttentionWork(stream=7)
+    del work  # anywhere, as by the garbage collector during a capture: no call may synchronise now
+    assert not recorder.of("gift_attention_work_destroy")
+    other = gift.AttentionWork(stream=7)
+    assert recorder.of("gift_attention_work_destroy") == [100] and other.handle == 101
+    third = gift.AttentionWork(stream=7)
+    del third
+    other.destroy()
+    assert sorted(recorder.of("gift_attention_work_destroy")) == [100, 101, 102]
+
+
+def test_a_workspace_that_was_never_made(recorder, monkeypatch):
+    monkeypatch.setattr(Recorder, "gift_attention_work_create", lambda self, stream, out: gift.E_NOMEM)
+    with pytest.raises(gift.GiftError):
+        gift.AttentionWork(stream=7)
+    assert not recorder.of("gift_attention_work_destroy")

@@ -1,5 +1,7 @@
 """Calls on several streams at once, with one AttentionWork: columns that several workgroups share are joined in a workspace
 of the stream's own."""
+import gc
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -44,4 +46,31 @@ def test_one_workspace_object_on_three_streams():
     for w, g in zip(want, got):
         for out, lse in g:
             assert torch.equal(out, w[0]) and torch.equal(lse, w[1])
+    work.destroy()
+
+
+def test_a_workspace_dropped_during_a_capture():
+    call = Call(Batch([9000, 3], [3, 2], heads=2, group=4, dim=128, seed=3))
+    work, other = gift.AttentionWork(), [gift.AttentionWork()]
+    want = call(work)
+    call(other[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(work)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other.clear()
+        gc.collect()
+        got = call(work)
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        again = call(work)
+        assert torch.equal(again[0], want[0])
+        got[0].zero_()
+        got[1].zero_()
     work.destroy()
