@@ -123,8 +123,9 @@ typedef struct {
  * any, may differ from call to call), and a request whose table names a block
  * that another user's request takes is OWNER_MIXED.  Requests of one user may
  * then share a block.
- * Outputs must not overlap inputs (GIFT_E_INVALID), except that tables and
- * block_labels are both.
+ * Outputs must not overlap inputs or each other (GIFT_E_INVALID), except that
+ * tables and block_labels are both.  All arrays are aligned to their elements
+ * (GIFT_E_INVALID), here and in the calls below.
  * Errors: GIFT_E_INVALID (null arrays, block_tokens no power of two, n_reqs
  * or table_width 0 where the other is not, table_stride below table_width),
  * GIFT_E_TOO_LARGE (table_width * block_tokens or n_slots past 2^31 - 1).
@@ -152,7 +153,7 @@ typedef struct {
  * rows' numbers in index, only what was accepted reaches the cache.
  *   slots  device, n_slots; index  device, n_slots u32, or NULL.
  * Errors: GIFT_E_INVALID (null or unaligned arrays, strides no multiple of
- * 16, the format), GIFT_E_RANGE (chunks exceed cache_bytes), GIFT_E_TOO_LARGE
+ * 16, arrays that overlap the cache, the format), GIFT_E_RANGE (chunks exceed cache_bytes), GIFT_E_TOO_LARGE
  * (more than 2^31 - 1 slots or rows).
  */
 gift_status gift_kv_append(const gift_paged_kv* kv, const gift_kv_format* format, const int64_t* slots,
@@ -218,7 +219,8 @@ typedef struct {
  * (float16; m the largest score so far; weights under 2^-29 of the largest to
  * steps of 2^-39 of it), and the output is rounded once at the end.
  * The same inputs give the same bits.
- *   out must not overlap q, k, v or the cache.
+ *   out and lse must not overlap each other, the cache or any other array of
+ *   the call.
  * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, head counts,
  * layer, scale, the format), GIFT_E_RANGE (chunks exceed cache_bytes),
  * GIFT_E_TOO_LARGE (rows, or table_width * block_tokens, past 2^31 - 1).

@@ -27,7 +27,7 @@ bool add_ok(uint64_t a, uint64_t b, uint64_t* r) { return !__builtin_add_overflo
 
 bool pow2(uint64_t x) { return x != 0 && (x & (x - 1)) == 0; }
 
-bool unaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+bool unaligned(const void* p, uint32_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
 // A strided array in memory: count[d] steps of stride[d] bytes around rows of
 // row bytes.  False where the last byte's offset does not fit 64 bits.
@@ -52,6 +52,13 @@ struct Strided {
 bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   return na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
+
+struct Range {
+  const void* p;
+  uint64_t n;  // bytes
+};
+
+bool overlap(const Range& a, const Range& b) { return overlap(a.p, a.n, b.p, b.n); }
 
 // Rules of gift_kv_format within a gift_paged_kv; fills the kernels' view.
 gift_status check_format(const gift_paged_kv* kv, const gift_kv_format* f, KvView* view) {
@@ -134,19 +141,21 @@ gift_status gift_kv_tables(const gift_kv_step* step, hipStream_t stream) {
                    entries > UINT64_MAX / 4 || s.n_blocks > UINT64_MAX / 4))
     return report(GIFT_E_INVALID, "table sizes overflow");
   const uint64_t per = 4ull * s.n_reqs;
-  struct Range {
-    const void* p;
-    uint64_t n;
-  } const in[] = {{s.users, per}, {s.lens, per}, {s.new_lens, per}, {s.free_blocks, 4ull * s.n_free}},
-      out[] = {{s.tables, 4 * entries}, {s.block_labels, 4 * s.n_blocks}, {s.slots, 8 * s.n_slots},
-               {s.row_begin, per + 4},  {s.lens_out, per},                {s.taken, 4},
-               {s.verdicts, per}};
+  const Range in[] = {{s.users, per}, {s.lens, per}, {s.new_lens, per}, {s.free_blocks, 4ull * s.n_free}},
+              out[] = {{s.tables, 4 * entries}, {s.block_labels, 4 * s.n_blocks}, {s.slots, 8 * s.n_slots},
+                       {s.row_begin, per + 4},  {s.lens_out, per},                {s.taken, 4},
+                       {s.verdicts, per}};
   const int n_out = (int)(sizeof out / sizeof out[0]);
+  for (const Range& r : in)
+    if (r.n && unaligned(r.p, 4)) return report(GIFT_E_INVALID, "an array is not aligned to its elements");
+  for (const Range& r : out)
+    if (r.n && unaligned(r.p, r.p == s.slots ? 8 : 4))
+      return report(GIFT_E_INVALID, "an array is not aligned to its elements");
   for (int i = 0; i < n_out; i++) {
     for (const Range& r : in)
-      if (overlap(out[i].p, out[i].n, r.p, r.n)) return report(GIFT_E_INVALID, "an output overlaps an input");
+      if (overlap(out[i], r)) return report(GIFT_E_INVALID, "an output overlaps an input");
     for (int j = 0; j < i; j++)
-      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return report(GIFT_E_INVALID, "outputs overlap");
+      if (overlap(out[i], out[j])) return report(GIFT_E_INVALID, "outputs overlap");
   }
   hipError_t e = launch_kv_tables(TablesArgs{s, (uint32_t)__builtin_ctz(s.block_tokens)}, stream);
   return e == hipSuccess ? GIFT_OK : report_hip(e, "kv_tables");
@@ -161,6 +170,11 @@ gift_status gift_kv_append(const gift_paged_kv* kv, const gift_kv_format* format
   if (!rows) return report(GIFT_E_INVALID, "null rows");
   if (n_slots > kMost || rows->n_rows > kMost) return report(GIFT_E_TOO_LARGE, "more than 2^31 - 1 slots or rows");
   if (n_slots && !slots) return report(GIFT_E_INVALID, "null slots");
+  if (n_slots && (unaligned(slots, 8) || unaligned(index, 4)))
+    return report(GIFT_E_INVALID, "slots or index not aligned to its elements");
+  if (overlap(slots, 8 * n_slots, kv->base, kv->cache_bytes) ||
+      (index && overlap(index, 4 * n_slots, kv->base, kv->cache_bytes)))
+    return report(GIFT_E_INVALID, "slots or index overlaps the cache");
   if (n_slots && rows->n_rows) {
     if (!rows->k || !rows->v || unaligned(rows->k) || unaligned(rows->v))
       return report(GIFT_E_INVALID, "k or v null or not 16-byte aligned");
@@ -255,6 +269,9 @@ gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* k
   if (g.n_reqs && g.table_stride < g.table_width) return report(GIFT_E_INVALID, "table_stride below table_width");
   if (!g.k != !g.v) return report(GIFT_E_INVALID, "k and v must both be given or both be NULL");
   if (g.mask && g.mask_words == 0) return report(GIFT_E_INVALID, "mask_words must be >= 1 with a mask");
+  for (const void* p : {(const void*)g.lse, (const void*)g.row_begin, (const void*)g.lens, (const void*)g.tables,
+                        (const void*)g.mask, (const void*)g.verdicts})
+    if (unaligned(p, 4)) return report(GIFT_E_INVALID, "an array is not aligned to its elements");
   if (g.n_rows) {
     if (!g.q || !g.out || unaligned(g.q) || unaligned(g.k) || unaligned(g.v) || unaligned(g.out))
       return report(GIFT_E_INVALID, "q, k, v or out null or not 16-byte aligned");
@@ -271,13 +288,28 @@ gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* k
     if ((lo_n > 1 && lo < row) || (hi_n > 1 && hi < row + (lo_n > 1 ? lo * (lo_n - 1) : 0)))
       return report(GIFT_E_INVALID, "rows of out overlap");
     if (overlap(out.p, n_out, kv->base, kv->cache_bytes)) return report(GIFT_E_INVALID, "out overlaps the cache");
+    const Range lse{g.lse, g.lse ? 4 * heads_rows : 0};
+    if (overlap(lse, Range{kv->base, kv->cache_bytes}) || overlap(lse, Range{g.out, n_out}))
+      return report(GIFT_E_INVALID, "lse overlaps out or the cache");
     const Strided in[3] = {{g.q, row, {rows, g.n_heads, 1}, {g.q_row_stride, g.q_head_stride, 0}},
                            {g.k, row, {rows, kvh, 1}, {g.k_row_stride, g.k_head_stride, 0}},
                            {g.v, row, {rows, kvh, 1}, {g.v_row_stride, g.v_head_stride, 0}}};
     for (const Strided& x : in) {
       if (!x.extent(&n)) return report(GIFT_E_INVALID, "sizes of q, k or v overflow");
       if (overlap(out.p, n_out, x.p, n)) return report(GIFT_E_INVALID, "out overlaps q, k or v");
+      if (overlap(lse, Range{x.p, n})) return report(GIFT_E_INVALID, "lse overlaps q, k or v");
     }
+    uint64_t entries = 0, words = 0;
+    if (g.n_reqs && g.table_width &&
+        (!mul_ok(g.table_stride, g.n_reqs - 1, &entries) || !add_ok(entries, g.table_width, &entries)))
+      return report(GIFT_E_INVALID, "sizes overflow");
+    if (g.mask && !mul_ok(rows, g.mask_words, &words)) return report(GIFT_E_INVALID, "sizes overflow");
+    if (entries > UINT64_MAX / 4 || words > UINT64_MAX / 4) return report(GIFT_E_INVALID, "sizes overflow");
+    const uint64_t per = 4ull * g.n_reqs;
+    for (const Range& r : {Range{g.row_begin, g.n_reqs ? per + 4 : 0}, Range{g.lens, per}, Range{g.tables, 4 * entries},
+                           Range{g.mask, 4 * words}, Range{g.verdicts, g.verdicts ? per : 0}})
+      if (overlap(lse, r) || overlap(Range{g.out, n_out}, r))
+        return report(GIFT_E_INVALID, "out or lse overlaps row_begin, lens, tables, mask or verdicts");
   }
   int dev;
   hipError_t e = hipGetDevice(&dev);
