@@ -223,7 +223,8 @@ typedef struct {
  *   the call.
  * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, head counts,
  * layer, scale, the format), GIFT_E_RANGE (chunks exceed cache_bytes),
- * GIFT_E_TOO_LARGE (rows, or table_width * block_tokens, past 2^31 - 1).
+ * GIFT_E_TOO_LARGE (rows, or table_width * block_tokens, past 2^31 - 1, or
+ * n_rows * n_heads past 2^32 - 1).
  */
 gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* kv, const gift_kv_format* format,
                                 const gift_tree_attention_args* args, hipStream_t stream);

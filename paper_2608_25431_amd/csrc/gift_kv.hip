@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "gift_kv_internal.hpp"
+#include "gift_kv_units.hpp"
 
 namespace gift {
 namespace {
@@ -418,24 +419,6 @@ __device__ inline Req req_at(const AttnArgs& p, const Said& s, uint32_t i) {
   return r;
 }
 
-// a / b: the usual small a by way of floats, which takes a fraction of the steps of a 32-bit division.  Exact: below 2^23
-// the product is off by less than the distance of a quotient from the next.
-__device__ inline uint32_t quotient(uint32_t a, uint32_t b) {
-  if (a >= 1u << 23) return a / b;
-  const float q = (float)a * __builtin_amdgcn_rcpf((float)b);
-  uint32_t n = (uint32_t)q;
-  const int32_t left = (int32_t)(a - n * b);
-  return left < 0 ? n - 1 : (uint32_t)left >= b ? n + 1 : n;
-}
-
-// a / b for a < 2^53, with the reciprocal of b
-__device__ inline uint64_t quotient(uint64_t a, uint64_t b, double reciprocal) {
-  uint64_t q = (uint64_t)((double)a * reciprocal);
-  if (q * b > a) q--;
-  if (a - q * b >= b) q++;
-  return q;
-}
-
 // Running state of one wave's 32 columns: lane l holds column l % 32; of O^T
 // the elements d = 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
 template <class S>
@@ -647,8 +630,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(AttnArgs p
       }
       r = req_at<S>(p, said, bi);
     }
-    const uint32_t at = (uint32_t)(unit - base), column = __builtin_amdgcn_readfirstlane(quotient(at, r.rounds)),
-                   it0 = at - column * r.rounds;
+    const Unit at = unit_of(unit - base, r.rounds);
+    const uint32_t column = __builtin_amdgcn_readfirstlane(at.column), it0 = __builtin_amdgcn_readfirstlane(at.round);
     const uint64_t col_first = unit - it0, col_last = col_first + r.rounds - 1;
     const uint32_t it1 = (uint32_t)(unit_end - unit < r.rounds - it0 ? it0 + (unit_end - unit) : r.rounds);
     const uint32_t g = __builtin_amdgcn_readfirstlane(quotient(column, r.col_tiles)), ct = column - g * r.col_tiles;

@@ -261,8 +261,8 @@ gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* k
   uint64_t tokens, heads_rows;
   if (!mul_ok(g.table_width, format->block_tokens, &tokens) || tokens > kMost)
     return report(GIFT_E_TOO_LARGE, "table_width * block_tokens exceeds 2^31 - 1");
-  if (!mul_ok(g.n_rows, g.n_heads, &heads_rows) || heads_rows > UINT64_MAX / 4)
-    return report(GIFT_E_INVALID, "sizes overflow");
+  if (!mul_ok(g.n_rows, g.n_heads, &heads_rows) || heads_rows > UINT32_MAX)
+    return report(GIFT_E_TOO_LARGE, "n_rows * n_heads exceeds 2^32 - 1");
   if (g.n_reqs > kMost) return report(GIFT_E_TOO_LARGE, "n_reqs exceeds 2^31 - 1");
   if (g.n_reqs && (!g.row_begin || !g.lens)) return report(GIFT_E_INVALID, "null row_begin or lens");
   if (g.n_reqs && g.table_width && !g.tables) return report(GIFT_E_INVALID, "null tables");
