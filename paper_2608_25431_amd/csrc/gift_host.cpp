@@ -1510,6 +1510,12 @@ gift_status report_hip(hipError_t e, const char* what) noexcept {
   }
 }
 
-gift_status paged_geometry(const gift_paged_kv* kv) { return check_paged_geometry(kv); }
+gift_status paged_geometry(const gift_paged_kv* kv) noexcept {
+  try {
+    return check_paged_geometry(kv);
+  } catch (...) {  // no memory for the message of a refusal
+    return GIFT_E_INVALID;
+  }
+}
 
 }  // namespace gift

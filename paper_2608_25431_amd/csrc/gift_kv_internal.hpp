@@ -13,7 +13,7 @@ namespace gift {
 void clear_error() noexcept;
 gift_status report(gift_status s, const char* message) noexcept;
 gift_status report_hip(hipError_t e, const char* what) noexcept;
-gift_status paged_geometry(const gift_paged_kv* kv);
+gift_status paged_geometry(const gift_paged_kv* kv) noexcept;
 
 // Where K and V of a layer's (block, token, head) lie.
 struct KvView {
