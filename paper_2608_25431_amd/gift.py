@@ -456,7 +456,8 @@ def kv_format(dtype, n_heads, head_dim, block_tokens, token_stride, head_stride,
 
 
 def _ints(x, n, name, size=4):
-    """Address of a device array of n integers of size bytes (a contiguous tensor of that width, or an address)."""
+    """Address of a device array of n integers of size bytes (a contiguous tensor of that width, or an address; None is
+    NULL)."""
     try:
         if x.is_cuda and x.element_size() == size and x.numel() >= n and x.is_contiguous():
             return x.data_ptr()
@@ -464,7 +465,7 @@ def _ints(x, n, name, size=4):
             raise ValueError(f"{name}: elements of {x.element_size()} bytes, the call needs {size}")
     except AttributeError:
         pass
-    return _dev(x, size * n, name)
+    return _dev(x, size * n, name) or 0
 
 
 def _matrix(x, rows, name):

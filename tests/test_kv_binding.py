@@ -100,3 +100,11 @@ def test_a_workspace_that_was_never_made(recorder, monkeypatch):
     with pytest.raises(gift.GiftError):
         gift.AttentionWork(stream=7)
     assert not recorder.of("gift_attention_work_destroy")
+
+
+def test_missing_arrays_are_refused_by_the_library():
+    with pytest.raises(gift.GiftError, match="null"):
+        attend(row_begin=None, verdicts=None)
+    one = Fake((3,), I)
+    with pytest.raises(gift.GiftError, match="null row_begin or taken"):
+        gift.kv_tables(one, one, one, 16, one, Fake((3, 5), I), one, Fake((9,), torch.int64), None, one, one, one, stream=0)
