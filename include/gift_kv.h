@@ -166,7 +166,8 @@ typedef struct gift_attention_work_s* gift_attention_work;
 
 /* Allocates a workspace on the current device and clears what must start
  * clear, on `stream`, which is synchronised before return.
- * Errors: GIFT_E_INVALID (null out), GIFT_E_NOMEM, GIFT_E_HIP. */
+ * Errors: GIFT_E_INVALID (null out, a stream that is being captured),
+ * GIFT_E_NOMEM, GIFT_E_HIP. */
 gift_status gift_attention_work_create(hipStream_t stream, gift_attention_work* out);
 
 /* Frees it; synchronises the device first.  NULL is a no-op. */

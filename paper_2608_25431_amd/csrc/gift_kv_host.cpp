@@ -207,6 +207,11 @@ gift_status gift_attention_work_create(hipStream_t stream, gift_attention_work* 
   int dev;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return report_hip(e, "hipGetDevice");
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  e = hipStreamIsCapturing(stream, &capture);
+  if (e != hipSuccess) return report_hip(e, "hipStreamIsCapturing");
+  // an allocation and a synchronisation would end the capture
+  if (capture != hipStreamCaptureStatusNone) return report(GIFT_E_INVALID, "the stream is being captured");
   int cus = 0;
   e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return report_hip(e, "hipDeviceGetAttribute");

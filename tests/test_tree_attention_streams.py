@@ -74,3 +74,21 @@ def test_a_workspace_dropped_during_a_capture():
         got[0].zero_()
         got[1].zero_()
     work.destroy()
+
+
+def test_no_workspace_is_made_during_a_capture():
+    call = Call(Batch([9000, 3], [3, 2], heads=2, group=4, dim=128, seed=4))
+    work = gift.AttentionWork()
+    want = call(work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(gift.GiftError, match="being captured"):
+            gift.AttentionWork()
+        got = call(work)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        got[0].zero_()
+    work.destroy()
