@@ -76,7 +76,7 @@ typedef struct {
   uint32_t* tables;              /* device, in and out */
   uint32_t* block_labels;        /* device, n_blocks, in and out */
   int64_t* slots;                /* device, n_slots, out */
-  uint64_t n_slots;              /* < 2^32 */
+  uint64_t n_slots;              /* < 2^31 */
   uint32_t* row_begin;           /* device, n_reqs + 1, out */
   uint32_t* lens_out;            /* device, n_reqs, out */
   uint32_t* taken;               /* device, 1, out */
@@ -211,9 +211,11 @@ typedef struct {
  * a row that sees nothing gets out = 0 and lse = -inf.  So do the rows of a
  * request whose verdict is not OK and rows that belong to no request.  What a
  * row does not see has no part in it, whatever it holds (NaN and infinities
- * included).  A table entry outside the cache is not followed: its tokens are
- * not seen.  lens past table_width * block_tokens are cut to it; row_begin is
- * taken as rising and cut to n_rows.
+ * included); an element of V that it sees and that is not finite makes that
+ * element of out not finite.  A table entry outside the cache is not followed:
+ * its tokens are not seen.  lens past table_width * block_tokens are cut to
+ * it; row_begin is taken as rising and cut to n_rows (where it falls, rows
+ * that two requests claim, or one and nobody, hold what either writes).
  * Scores, maxima, sums and the running output are 32-bit floats; for the
  * product with V the weights exp(s_j - m) are rounded to 16 significant bits
  * (bfloat16, in two parts; m at most 5.6 below the largest score) or to 11

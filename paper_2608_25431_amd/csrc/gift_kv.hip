@@ -486,7 +486,7 @@ __device__ inline float max_of_halves(float x) {
 // elements, 537 MB) take 111 us, 4.8 TB/s, which is what a large copy reaches.
 // With many rows by what a wave does one after the other: 32 requests of
 // 2048-8192 tokens with trees of 16-32 tokens and 64 heads (729 MB, 142 GFLOP)
-// take 286 us.  Without products and exponentials the loads and stores alone take
+// take 290 us.  Without products and exponentials the loads and stores alone take
 // 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
 // two waves a SIMD that meet once a round hide a third of that.
 template <class E, class S, int MINW>
