@@ -122,7 +122,8 @@ typedef struct {
  * users that the list gives the same id one at most gets it (which one, if
  * any, may differ from call to call), and a request whose table names a block
  * that another user's request takes is OWNER_MIXED.  Requests of one user may
- * then share a block.
+ * then share a block, and the verdict of one whose table names it may be
+ * either.
  * Outputs must not overlap inputs or each other (GIFT_E_INVALID), except that
  * tables and block_labels are both.  All arrays are aligned to their elements
  * (GIFT_E_INVALID), here and in the calls below.
