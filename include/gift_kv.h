@@ -36,8 +36,10 @@ extern "C" {
  * of the table, the free list or the slot array is too short for them). */
 enum { GIFT_SEG_NO_SPACE = 3 };
 
-/* Element types of K, V, queries and outputs. */
-enum { GIFT_BF16 = 1, GIFT_F16 = 2 };
+/* Element types of K, V, queries and outputs; of a quantised cache alone (the
+ * calls with gift_kv_scales): GIFT_E4M3, 8 bits with 4 of exponent and 3 of
+ * mantissa, largest 448, no infinities. */
+enum { GIFT_BF16 = 1, GIFT_F16 = 2, GIFT_E4M3 = 3 };
 
 /*
  * How the tokens lie within a (layer, block) of a gift_paged_kv: K of token t
@@ -232,6 +234,160 @@ typedef struct {
  */
 gift_status gift_tree_attention(gift_attention_work work, const gift_paged_kv* kv, const gift_kv_format* format,
                                 const gift_tree_attention_args* args, hipStream_t stream);
+
+/* Queries and keys on their way from a projection to the cache and to the
+ * attention. */
+typedef struct {
+  uint64_t n_rows;
+  uint32_t q_heads, k_heads; /* either may be 0: then its arrays are not used */
+  uint32_t head_dim;         /* 64, 96, 128 or 256 */
+  uint32_t dtype;            /* GIFT_BF16 or GIFT_F16: rows and weights */
+  const void *q, *k;         /* device; [n_rows][heads][head_dim] */
+  void *q_out, *k_out;       /* device; likewise; q and k themselves are allowed, with the same strides */
+  uint64_t q_row_stride, q_head_stride; /* bytes, multiples of 16, as all that follow */
+  uint64_t k_row_stride, k_head_stride;
+  uint64_t q_out_row_stride, q_out_head_stride;
+  uint64_t k_out_row_stride, k_out_head_stride;
+  const void *q_weight, *k_weight; /* device, head_dim elements, 16-byte aligned; NULL: not normalised */
+  float eps;                 /* >= 0, finite */
+  uint32_t rotary_dim;       /* elements of a head that are rotated, its first ones; a multiple of 16, or 0 */
+  uint32_t interleaved;      /* pairs (2i, 2i + 1); 0: (i, i + rotary_dim / 2) */
+  uint32_t n_axes;           /* 1 to 4 */
+  uint32_t sections[4];      /* pairs that turn by each axis, one section after the other; rotary_dim / 2 in all */
+  const float* inv_freq;     /* device, rotary_dim / 2: radians per position */
+  const int32_t* positions;  /* device, [n_axes][position_stride] */
+  uint64_t position_stride;  /* entries, >= n_rows where n_axes > 1 */
+} gift_qk_rows;
+
+/*
+ * The norm of every head's query and key and the rotation by its token's
+ * position, in one pass:
+ *     y = x * weight / sqrt(mean(x^2) + eps)          (where there is a weight)
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t) of each pair i of y,
+ *     t = positions[axis of i][row] * inv_freq[i]
+ * All in 32-bit floats, rounded once at the end; the number of turns of an
+ * angle is taken in 64 bits, so that far positions keep theirs.
+ * Outputs overlap nothing else that the call uses (GIFT_E_INVALID), except
+ * that q_out may be q and k_out may be k; queries and keys may lie in one
+ * buffer, those of a row beside each other.
+ * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, sizes, sections,
+ * eps, overlaps), GIFT_E_TOO_LARGE (n_rows past 2^31 - 1, or
+ * n_rows * (q_heads + k_heads) past 2^32 - 1).
+ */
+gift_status gift_qk_norm_rope(const gift_qk_rows* rows, hipStream_t stream);
+
+/*
+ * A quantised cache: elements of GIFT_E4M3 as a gift_paged_kv and a
+ * gift_kv_format describe them (a row is head_dim bytes), and for each 32
+ * elements of a row a byte b: the element e stands for e * 2^(b - 127).  These
+ * bytes lie in a paged cache of their own with as many layers and blocks, so
+ * that a block is sealed as two (gift_seal_paged of either): those of token
+ * t's K in head h are the head_dim / 32 bytes at
+ *     base + layer*layer_stride + block*block_stride
+ *          + k_offset + t*token_stride + h*head_stride
+ * of `cache`, those of V likewise from v_offset.  A row of them takes 4 bytes,
+ * of head_dim 256 it takes 8; offsets and strides are multiples of that.  The
+ * rules for rows are those of gift_kv_format, and the two caches do not
+ * overlap (GIFT_E_INVALID).
+ */
+typedef struct {
+  gift_paged_kv cache;
+  uint64_t k_offset, v_offset;        /* bytes */
+  uint64_t token_stride, head_stride; /* bytes */
+} gift_kv_scales;
+
+/*
+ * gift_kv_append into a quantised cache: layers layer .. layer + n_layers - 1
+ * of it, from layers 0 .. n_layers - 1 of the rows, which are of `dtype`
+ * (GIFT_BF16 or GIFT_F16).  For 32 elements of a row with the largest finite
+ * magnitude x, b is the smallest byte with x <= 448 * 2^(b - 127), at least 27;
+ * each element is divided by 2^(b - 127) and rounded to the nearest element,
+ * ties to even.  What would be past the range of the rows' type when read back
+ * becomes the largest element that is not (240 times the factor); NaN and
+ * infinities become NaN (0x7F with the sign).  The bytes of a row of factors
+ * past head_dim / 32 become 0.
+ * Errors: as gift_kv_append, and GIFT_E_INVALID for layers past the cache's.
+ */
+gift_status gift_kv_append_quant(const gift_paged_kv* kv, const gift_kv_format* format, const gift_kv_scales* scales,
+                                 uint32_t layer, uint32_t n_layers, const int64_t* slots, uint64_t n_slots,
+                                 const uint32_t* index, const gift_kv_rows* rows, uint32_t dtype, hipStream_t stream);
+
+/* Cached tokens of requests as rows: element 0 of layer l, row r, head h goes
+ * to k + l*k_layer_stride + r*k_row_stride + h*k_head_stride; V likewise. */
+typedef struct {
+  void *k, *v;               /* device, 16-byte aligned */
+  uint64_t n_rows;           /* < 2^31 */
+  uint64_t k_layer_stride, k_row_stride, k_head_stride; /* bytes, multiples of 16 */
+  uint64_t v_layer_stride, v_row_stride, v_head_stride;
+  uint32_t dtype;            /* GIFT_BF16 or GIFT_F16 */
+  uint32_t layer, n_layers;  /* layers layer .. layer + n_layers - 1 of the cache */
+  uint32_t n_reqs;
+  const uint32_t* row_begin; /* device, n_reqs + 1: request b has rows row_begin[b] .. row_begin[b+1] - 1 */
+  const uint32_t* first;     /* device, n_reqs: the token of a request's first row; NULL: 0 */
+  const uint32_t* lens;      /* device, n_reqs: cached tokens */
+  const uint32_t* tables;    /* device, [n_reqs][table_stride] */
+  uint32_t table_width;      /* entries of a row that may be used */
+  uint64_t table_stride;
+  const int32_t* verdicts;   /* device, n_reqs, or NULL: all OK */
+} gift_kv_read_args;
+
+/*
+ * Reads cached tokens of a quantised cache back in 16 bits: row i of request b
+ * gets token first[b] + i, each element e * 2^(b - 127) rounded to the type
+ * (exact in bfloat16 for what gift_kv_append_quant writes, in float16 for what
+ * it writes of float16 rows).  Rows past lens[b], of table entries outside the
+ * cache and of requests whose verdict is not OK get zeros; rows of no request
+ * stay as they are.  lens and row_begin are cut as in gift_tree_attention.
+ * k and v must not overlap any other array of the call, and no two of their
+ * rows overlap (sorted by stride, each is at least the extent of what is inside
+ * it; k and v lie apart, or in one buffer with the same strides).
+ * Errors: GIFT_E_INVALID (null or unaligned arrays, strides, layers, overlaps,
+ * the format), GIFT_E_RANGE (chunks exceed cache_bytes), GIFT_E_TOO_LARGE (rows,
+ * or table_width * block_tokens, past 2^31 - 1).
+ */
+gift_status gift_kv_read_quant(const gift_paged_kv* kv, const gift_kv_format* format, const gift_kv_scales* scales,
+                               const gift_kv_read_args* args, hipStream_t stream);
+
+typedef struct {
+  uint64_t n_rows;        /* rows of q and out, < 2^31 */
+  uint32_t n_reqs;
+  uint32_t n_heads;       /* query heads, a multiple of the format's n_heads */
+  uint32_t layer;         /* of the cache */
+  uint32_t dtype;         /* GIFT_BF16 or GIFT_F16: q and out */
+  float scale;            /* of the scores, finite; usually 1 / sqrt(head_dim) */
+  const void* q;          /* device; [n_rows][n_heads][head_dim] */
+  void* out;              /* device; as q */
+  float* lse;             /* device, [n_rows][n_heads] contiguous, or NULL */
+  uint64_t q_row_stride, q_head_stride;     /* bytes, multiples of 16, as all that follow */
+  uint64_t out_row_stride, out_head_stride;
+  const uint32_t* row_begin; /* device, n_reqs + 1: request b has rows row_begin[b] .. row_begin[b+1] - 1 */
+  const uint32_t* lens;      /* device, n_reqs: cached tokens, those of the request's rows among them */
+  const uint32_t* tables;    /* device, [n_reqs][table_stride] */
+  uint32_t table_width;      /* entries of a row that may be used */
+  uint64_t table_stride;
+  const uint32_t* mask;      /* device, [n_rows][mask_words], or NULL */
+  uint32_t mask_words;
+  const int32_t* verdicts;   /* device, n_reqs, or NULL: all OK */
+} gift_quant_attention_args;
+
+/*
+ * gift_tree_attention over a quantised cache, whose last tokens are the rows'
+ * own: gift_kv_append_quant writes a step's tokens before their attention
+ * (rejected drafts are written over by the next step's).  With lens[b] cached
+ * tokens (cut to table_width * block_tokens) and R rows, row i of request b is
+ * token lens[b] - R + i, and sees
+ *   - all tokens before lens[b] - R, and
+ *   - token lens[b] - R + j if bit j % 32 of word j / 32 of its row of the mask
+ *     is set; rows past 32 * mask_words are not seen; without a mask, j <= i.
+ * K and V are the values of the cache's elements in the type of q, as
+ * gift_kv_read_quant gives them (factor bytes 0 and 255, which are never
+ * written, give values that are not defined).  All else, roundings among it, is
+ * as in gift_tree_attention: rows that see nothing, verdicts, table entries
+ * outside the cache, what is not seen, workspaces, overlaps and errors.
+ */
+gift_status gift_quant_attention(gift_attention_work work, const gift_paged_kv* kv, const gift_kv_format* format,
+                                 const gift_kv_scales* scales, const gift_quant_attention_args* args,
+                                 hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgift.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("gift_kernels.hip", "gift_host.cpp", "gift_ift.cpp", "gift_kv.hip",
+SOURCES = [os.path.join(CSRC, f) for f in ("gift_kernels.hip", "gift_host.cpp", "gift_ift.cpp", "gift_kv.hip", "gift_kv_quant.hip",
                                            "gift_kv_host.cpp")]
 PROBE_SOURCE = os.path.join(CSRC, "gift_probe.hip")
 PROBE_LIB = os.path.join(HERE, "libgift_probe.so")

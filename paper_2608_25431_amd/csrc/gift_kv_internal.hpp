@@ -44,6 +44,10 @@ struct AttnArgs {
   gift_tree_attention_args a;
   uint32_t group;  // query heads of a KV head
 };
+// The same over a quantised cache: kv is of its elements, of one byte each, and the drafted rows of `a` are NULL.
+struct QuantAttnArgs : AttnArgs {
+  KvView scales;
+};
 // The attention's workspace: counters of the columns that are joined and of
 // runs of their parts (zero between calls: the workgroup that counts a last
 // part clears the counter), a quarter and a half of them, then two places per
@@ -57,5 +61,23 @@ struct AttnWork {
   size_t partial_bytes;  // past the counters
 };
 hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
+hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
+
+hipError_t launch_qk_norm_rope(const gift_qk_rows& a, hipStream_t s);
+
+struct QuantAppendArgs {
+  KvView kv, scales;  // bases: of layer 0
+  gift_kv_rows src;
+  const int64_t* slots;
+  const uint32_t* index;
+  uint32_t n_slots, layer, n_layers;
+};
+hipError_t launch_kv_append_quant(const QuantAppendArgs& a, uint32_t dtype, hipStream_t s);
+
+struct QuantReadArgs {
+  KvView kv, scales;
+  gift_kv_read_args a;
+};
+hipError_t launch_kv_read_quant(const QuantReadArgs& a, hipStream_t s);
 
 }  // namespace gift

@@ -23,7 +23,7 @@ LIB_PATH = os.path.join(HERE, "libgift.so")
 OK, E_INVALID, E_RANGE, E_OVERLAP, E_NONCE_REUSE, E_TOO_LARGE, E_HIP, E_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7
 E_REJECTED, E_RACE = -8, -9
 SEG_OK, SEG_AUTH_FAIL, SEG_OWNER_MIXED, SEG_NO_SPACE = 0, 1, 2, 3
-BF16, F16 = 1, 2
+BF16, F16, E4M3 = 1, 2, 3
 LABEL_PARAM, LABEL_UNOWNED = 0xFFFFFFFE, 0xFFFFFFFF
 
 # Host layout of gift_segment (32 bytes).
@@ -96,6 +96,39 @@ class _TreeAttention(ctypes.Structure):
          ("mask_words", ctypes.c_uint32), ("verdicts", ctypes.c_void_p)]
 
 
+class _QkRows(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_uint64), ("q_heads", ctypes.c_uint32), ("k_heads", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32), ("dtype", ctypes.c_uint32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p)] + \
+        [(f"{x}_{d}_stride", ctypes.c_uint64) for x in ("q", "k", "q_out", "k_out") for d in ("row", "head")] + \
+        [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+         ("rotary_dim", ctypes.c_uint32), ("interleaved", ctypes.c_uint32), ("n_axes", ctypes.c_uint32),
+         ("sections", ctypes.c_uint32 * 4), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+         ("position_stride", ctypes.c_uint64)]
+
+
+class _KvScales(ctypes.Structure):
+    _fields_ = [("cache", _PagedKV), ("k_offset", ctypes.c_uint64), ("v_offset", ctypes.c_uint64),
+                ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class _KvRead(ctypes.Structure):
+    _fields_ = _KvRows._fields_ + \
+        [("dtype", ctypes.c_uint32), ("layer", ctypes.c_uint32), ("n_layers", ctypes.c_uint32), ("n_reqs", ctypes.c_uint32),
+         ("row_begin", ctypes.c_void_p), ("first", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("tables", ctypes.c_void_p),
+         ("table_width", ctypes.c_uint32), ("table_stride", ctypes.c_uint64), ("verdicts", ctypes.c_void_p)]
+
+
+class _QuantAttention(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_uint64), ("n_reqs", ctypes.c_uint32), ("n_heads", ctypes.c_uint32),
+                ("layer", ctypes.c_uint32), ("dtype", ctypes.c_uint32), ("scale", ctypes.c_float), ("q", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p)] + \
+        [(f"{x}_{d}_stride", ctypes.c_uint64) for x in ("q", "out") for d in ("row", "head")] + \
+        [("row_begin", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("tables", ctypes.c_void_p),
+         ("table_width", ctypes.c_uint32), ("table_stride", ctypes.c_uint64), ("mask", ctypes.c_void_p),
+         ("mask_words", ctypes.c_uint32), ("verdicts", ctypes.c_void_p)]
+
+
 assert ctypes.sizeof(_Segment) == SEGMENT_DTYPE.itemsize == 32
 
 EXPORTS = ("gift_key_table_create", "gift_key_table_users", "gift_key_table_destroy", "gift_seal", "gift_seal_noalloc",
@@ -104,7 +137,7 @@ EXPORTS = ("gift_key_table_create", "gift_key_table_users", "gift_key_table_dest
            "gift_status_string", "gift_last_error",
            # include/gift_kv.h
            "gift_kv_tables", "gift_kv_append", "gift_attention_work_create", "gift_attention_work_destroy",
-           "gift_tree_attention",
+           "gift_tree_attention", "gift_qk_norm_rope", "gift_kv_append_quant", "gift_kv_read_quant", "gift_quant_attention",
            # include/gift_ift.h
            "gift_own_create", "gift_own_destroy", "gift_own_register", "gift_own_release", "gift_own_units",
            "gift_own_flat_index", "gift_own_set", "gift_own_get", "gift_own_labels", "gift_own_ops",
@@ -158,6 +191,16 @@ def lib():
         L.gift_tree_attention.argtypes = [P, ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat),
                                           P, P]
         L.gift_tree_attention.restype = st
+        cache = [ctypes.POINTER(_PagedKV), ctypes.POINTER(_KvFormat), ctypes.POINTER(_KvScales)]
+        L.gift_qk_norm_rope.argtypes = [P, P]
+        L.gift_qk_norm_rope.restype = st
+        L.gift_kv_append_quant.argtypes = cache + [ctypes.c_uint32, ctypes.c_uint32, P, ctypes.c_uint64, P, P, ctypes.c_uint32,
+                                                   P]
+        L.gift_kv_append_quant.restype = st
+        L.gift_kv_read_quant.argtypes = cache + [P, P]
+        L.gift_kv_read_quant.restype = st
+        L.gift_quant_attention.argtypes = [P, *cache, P, P]
+        L.gift_quant_attention.restype = st
         L.gift_profile_next_call.argtypes = [P, P]
         L.gift_profile_next_call.restype = st
         L.gift_status_string.argtypes = [st]
@@ -434,7 +477,7 @@ def token_decrypt(segs, blocks, n_tokens, kt, eos_token, tokens_out, nonces_out=
 def _types():
     """Codes of the element types K and V may have, by torch's type."""
     import torch
-    return {torch.bfloat16: BF16, torch.float16: F16}
+    return {torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3}
 
 
 _codes = None
@@ -448,10 +491,11 @@ def _code(dtype):
 
 
 def kv_format(dtype, n_heads, head_dim, block_tokens, token_stride, head_stride, v_offset, k_offset=0):
-    """gift_kv_format.  dtype: torch.bfloat16, torch.float16 or their codes (BF16, F16); offsets and strides in bytes."""
+    """gift_kv_format.  dtype: torch.bfloat16, torch.float16 or their codes (BF16, F16), or torch.float8_e4m3fn or E4M3 for a
+    quantised cache (kv_scales()); offsets and strides in bytes."""
     code = dtype if isinstance(dtype, int) else _code(dtype)
     if code is None:
-        raise ValueError(f"dtype {dtype}: K and V are bfloat16 or float16")
+        raise ValueError(f"dtype {dtype}: K and V are bfloat16 or float16, or float8_e4m3fn in a quantised cache")
     return _KvFormat(code, n_heads, head_dim, block_tokens, k_offset, v_offset, token_stride, head_stride)
 
 
@@ -485,10 +529,33 @@ def _rows_of(x, fmt, want, name):
         raise ValueError(f"{name}: tensor must be on the GPU")
     if _code(x.dtype) != fmt.dtype:
         raise ValueError(f"{name}: {x.dtype} is not the cache's type")
+    return _strided(x, want, name)
+
+
+def _rows_like(x, code, want, name):
+    """As _rows_of, of a type by its code."""
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name}: tensor must be on the GPU")
+    if _code(x.dtype) != code:
+        raise ValueError(f"{name}: {x.dtype} is not the other rows' type")
+    return _strided(x, want, name)
+
+
+def _code16(x, name):
+    """The code of a tensor's 16-bit type."""
+    code = _code(getattr(x, "dtype", None))
+    if code != BF16 and code != F16:
+        raise ValueError(f"{name}: needs a tensor of bfloat16 or float16")
+    return code
+
+
+def _strided(x, want, name):
     if x.shape != want:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {want}")
     strides = x.stride()
     if strides[-1] != 1:
+        if 0 in want:  # nothing in it: its strides say nothing
+            return x.data_ptr(), [0] * (len(want) - 1)
         raise ValueError(f"{name}: the last dimension must be contiguous")
     return x.data_ptr(), [2 * s for s in strides[:-1]] if min(want) > 1 else \
         [2 * s if n > 1 else 0 for n, s in zip(want, strides[:-1])]
@@ -503,7 +570,11 @@ def _same_format(kv, fmt):
 _STEP = struct.Struct("@IIQPPPPIIQPPPQPPPP")
 _ROWS = struct.Struct("@PPQ6Q")
 _TREE = struct.Struct("@QIIIfPPPPP8QPPPIQPIP")
-assert (_STEP.size, _ROWS.size, _TREE.size) == tuple(map(ctypes.sizeof, (_KvStep, _KvRows, _TreeAttention)))
+_QK = struct.Struct("@QIIIIPPPP8QPPfIII4IPPQ")
+_READ = struct.Struct("@PPQ6QIIIIPPPPIQP")
+_QUANT = struct.Struct("@QIIIIfPPP4QPPPIQPIP")
+assert (_STEP.size, _ROWS.size, _TREE.size, _QK.size, _READ.size, _QUANT.size) == \
+    tuple(map(ctypes.sizeof, (_KvStep, _KvRows, _TreeAttention, _QkRows, _KvRead, _QuantAttention)))
 
 
 def kv_tables(users, lens, new_lens, block_tokens, free_blocks, tables, block_labels, slots, row_begin, lens_out, taken,
@@ -591,6 +662,18 @@ class AttentionWork:
             pass
 
 
+def _mask(mask, rows):
+    """Address and words a row of a mask, of which None is no mask."""
+    if mask is None:
+        return 0, 0
+    if len(mask.shape) != 2 or mask.shape[0] < rows:
+        raise ValueError(f"mask: needs {rows} rows of words")
+    words = mask.shape[1]
+    if rows and words == 0:  # its address would be NULL, which stands for no mask
+        raise ValueError("mask: needs at least one word a row")
+    return _ints(mask, rows * words, "mask"), words
+
+
 def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, mask=None, verdicts=None, lse=None,
                    scale=None, stream=None):
     """gift_tree_attention.  q, out device tensors [n_rows][n_heads][head_dim]; k, v [n_rows][kv heads][head_dim], or
@@ -609,14 +692,7 @@ def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, 
     if v is not None:
         vp, vs = _rows_of(v, fmt, (rows, fmt.n_heads, dim), "v")
     tab, width, stride = _matrix(tables, n, "tables")
-    words = mp = 0
-    if mask is not None:
-        if len(mask.shape) != 2 or mask.shape[0] < rows:
-            raise ValueError(f"mask: needs {rows} rows of words")
-        words = mask.shape[1]
-        if rows and words == 0:  # its address would be NULL, which stands for no mask
-            raise ValueError("mask: needs at least one word a row")
-        mp = _ints(mask, rows * words, "mask")
+    mp, words = _mask(mask, rows)
     a = _TREE.pack(rows, n, heads, layer, dim ** -0.5 if scale is None else scale, qp, kp, vp, op,
                    0 if lse is None else _ints(lse, rows * heads, "lse"), *qs, *ks, *vs, *os_,
                    _ints(row_begin, n + 1, "row_begin"), _ints(lens, n, "lens"), tab, width, stride, mp, words,
@@ -625,6 +701,134 @@ def tree_attention(work, kv, fmt, layer, q, k, v, row_begin, lens, tables, out, 
     if handle and stream != work.stream:
         handle = work.on(stream)
     _check(lib().gift_tree_attention(handle, kv, fmt, a, stream))
+
+
+def kv_scales(cache, v_offset, token_stride, head_stride, k_offset=0):
+    """gift_kv_scales.  cache from paged_kv(): where the factors of a quantised cache lie; offsets and strides in bytes."""
+    if not isinstance(cache, _PagedKV):
+        raise TypeError("cache comes from paged_kv()")
+    return _KvScales(cache, k_offset, v_offset, token_stride, head_stride)
+
+
+def _same_scales(kv, fmt, scales):
+    _same_format(kv, fmt)
+    if not isinstance(scales, _KvScales):
+        raise TypeError("scales come from kv_scales()")
+
+
+def qk_norm_rope(q, k, q_out, k_out, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, sections=None,
+                 interleaved=False, stream=None):
+    """gift_qk_norm_rope.  Device tensors: q, q_out [n_rows][heads][head_dim]; k, k_out likewise, or both None; any strides
+    but the last; an output may be its input.  q_weight, k_weight [head_dim] of the same type, or None: not normalised.
+    inv_freq float32 [rotary_dim / 2], or None: not rotated; positions int32 [n_rows], or [n_axes][n_rows] with sections, the
+    pairs of each axis."""
+    code, shape = _code16(q, "q"), q.shape
+    if len(shape) != 3:
+        raise ValueError(f"q: shape {tuple(shape)}, the call needs [n_rows][heads][head_dim]")
+    rows, heads, dim = shape
+    qp, qs = _rows_like(q, code, (rows, heads, dim), "q")
+    qo, qos = _rows_like(q_out, code, (rows, heads, dim), "q_out")
+    kp = ko = kv_heads = 0
+    ks = kos = (0, 0)
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out: both or neither")
+    if k is not None:
+        kv_heads = k.shape[1] if len(k.shape) == 3 else 0
+        kp, ks = _rows_like(k, code, (rows, kv_heads, dim), "k")
+        ko, kos = _rows_like(k_out, code, (rows, kv_heads, dim), "k_out")
+    weights = []
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            if _code16(w, name) != code:
+                raise ValueError(f"{name}: {w.dtype} is not the rows' type")
+            if w.numel() != dim:
+                raise ValueError(f"{name}: {w.numel()} elements, the call needs {dim}")
+            w = _dev(w, 2 * dim, name)
+        weights.append(w or 0)
+    turned = places = freq = stride = 0
+    axes, parts = 1, (0, 0, 0, 0)
+    if inv_freq is not None:
+        turned = 2 * inv_freq.numel()
+        freq = _floats(inv_freq, "inv_freq")
+        if positions is None:
+            raise ValueError("positions: needed with inv_freq")
+        axes = positions.shape[0] if len(positions.shape) == 2 else 1
+        if len(positions.shape) not in (1, 2) or positions.shape[-1] < rows or not 1 <= axes <= 4:
+            raise ValueError(f"positions: shape {tuple(positions.shape)}, the call needs {rows} a row, of 1 to 4 axes")
+        if not positions.is_cuda or positions.element_size() != 4 or positions.dtype.is_floating_point or \
+                (positions.shape[-1] > 1 and positions.stride(-1) != 1):
+            raise ValueError("positions: needs adjacent int32 on the GPU")
+        stride = positions.stride(0) if axes > 1 else positions.shape[-1]
+        places = positions.data_ptr()
+        parts = [inv_freq.numel()] if sections is None and axes == 1 else list(sections or ())
+        if len(parts) != axes or min(parts) < 0:
+            raise ValueError(f"sections: needs the pairs of {axes} axes")
+        parts += [0] * (4 - axes)
+    a = _QK.pack(rows, heads, kv_heads, dim, code, qp, kp, qo, ko, *qs, *ks, *qos, *kos, *weights, eps, turned,
+                 int(bool(interleaved)), axes, *parts, freq, places, stride)
+    _check(lib().gift_qk_norm_rope(a, _stream(stream)))
+
+
+def _floats(x, name):
+    """Address of a contiguous float32 tensor on the GPU."""
+    if not x.is_cuda or not x.is_contiguous() or x.element_size() != 4 or not x.dtype.is_floating_point:
+        raise ValueError(f"{name}: needs a contiguous float32 tensor on the GPU")
+    return x.data_ptr()
+
+
+def kv_append_quant(kv, fmt, scales, slots, k, v, layer=0, index=None, stream=None):
+    """gift_kv_append_quant.  kv, fmt, scales of a quantised cache; slots device int64 [n_slots]; k, v device tensors of
+    bfloat16 or float16, [n_layers][n_rows][heads][head_dim], any strides but the last: layers layer .. layer + n_layers - 1 of
+    the cache; index device int32 [n_slots] or None."""
+    _same_scales(kv, fmt, scales)
+    n, code = slots.numel(), _code16(k, "k")
+    layers, rows = k.shape[:2] if len(k.shape) == 4 else (0, 0)
+    want = (layers, rows, fmt.n_heads, fmt.head_dim)
+    kp, ks = _rows_like(k, code, want, "k")
+    vp, vs = _rows_like(v, code, want, "v")
+    if index is None and rows < n:
+        raise ValueError(f"k: {rows} rows, the call needs {n}")
+    _check(lib().gift_kv_append_quant(kv, fmt, scales, layer, layers, _ints(slots, n, "slots", 8), n,
+                                      None if index is None else _ints(index, n, "index"),
+                                      _ROWS.pack(kp, vp, rows, *ks, *vs), code, _stream(stream)))
+
+
+def kv_read_quant(kv, fmt, scales, tables, lens, row_begin, k, v, layer=0, first=None, verdicts=None, stream=None):
+    """gift_kv_read_quant.  k, v device tensors of bfloat16 or float16, [n_layers][n_rows][heads][head_dim], any strides but
+    the last, from layers layer .. layer + n_layers - 1; row_begin int32 [n_reqs + 1]; lens, first, verdicts int32 [n_reqs];
+    tables int32 [n_reqs][width]."""
+    _same_scales(kv, fmt, scales)
+    n, code = lens.numel(), _code16(k, "k")
+    layers, rows = k.shape[:2] if len(k.shape) == 4 else (0, 0)
+    want = (layers, rows, fmt.n_heads, fmt.head_dim)
+    kp, ks = _rows_like(k, code, want, "k")
+    vp, vs = _rows_like(v, code, want, "v")
+    tab, width, stride = _matrix(tables, n, "tables")
+    a = _READ.pack(kp, vp, rows, *ks, *vs, code, layer, layers, n, _ints(row_begin, n + 1, "row_begin"),
+                   0 if first is None else _ints(first, n, "first"), _ints(lens, n, "lens"), tab, width, stride,
+                   0 if verdicts is None else _ints(verdicts, n, "verdicts"))
+    _check(lib().gift_kv_read_quant(kv, fmt, scales, a, _stream(stream)))
+
+
+def quant_attention(work, kv, fmt, scales, layer, q, row_begin, lens, tables, out, mask=None, verdicts=None, lse=None,
+                    scale=None, stream=None):
+    """gift_quant_attention.  kv, fmt, scales of a quantised cache that holds the rows' own tokens; q, out device tensors of
+    bfloat16 or float16, [n_rows][n_heads][head_dim], any strides but the last; the others as in tree_attention."""
+    _same_scales(kv, fmt, scales)
+    n, shape, code, dim = lens.numel(), q.shape, _code16(q, "q"), fmt.head_dim
+    rows, heads = (shape[0], shape[1]) if len(shape) == 3 else (0, 0)
+    qp, qs = _rows_like(q, code, (rows, heads, dim), "q")
+    op, os_ = _rows_like(out, code, (rows, heads, dim), "out")
+    tab, width, stride = _matrix(tables, n, "tables")
+    mp, words = _mask(mask, rows)
+    a = _QUANT.pack(rows, n, heads, layer, code, dim ** -0.5 if scale is None else scale, qp, op,
+                    0 if lse is None else _ints(lse, rows * heads, "lse"), *qs, *os_, _ints(row_begin, n + 1, "row_begin"),
+                    _ints(lens, n, "lens"), tab, width, stride, mp, words,
+                    0 if verdicts is None else _ints(verdicts, n, "verdicts"))
+    stream, handle = _stream(stream) or 0, work.handle
+    if handle and stream != work.stream:
+        handle = work.on(stream)
+    _check(lib().gift_quant_attention(handle, kv, fmt, scales, a, stream))
 
 
 def profile_next_call(before, after):

@@ -1,0 +1,230 @@
+"""Rows quantised into a paged cache, and cached tokens read back, against references in 64 bits: every byte is exact."""
+import numpy as np
+import pytest
+import torch
+
+from kv_helpers import DEV, DT, NO_BLOCK, i32
+from paper_2608_25431_amd import gift
+from quant_helpers import ELEMENTS, LARGEST, NAN, QuantCache, Requests, quantised, rounded, values
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_of(dtype, *shape, seed=0):
+    """Values of the type, of many magnitudes, with zeros and whole groups of them."""
+    r = np.random.default_rng(seed)
+    x = r.standard_normal(shape) * 2.0 ** r.integers(-12, 12, shape[:-1] + (1,))
+    x[..., ::7] *= 2.0 ** -6
+    x[r.random(shape) < 0.05] = 0
+    x[..., :32][r.random(shape[:-1]) < 0.1] = 0
+    return rounded(x, dtype)
+
+
+def append(cache, x, dtype, slots, layer=0, index=None, stream=None):
+    """x: (K and V, layers, rows, heads, dim)."""
+    k, v = torch.from_numpy(x).to(DEV, torch.float64).to(DT[dtype])
+    gift.kv_append_quant(*cache.args(), torch.from_numpy(np.asarray(slots, np.int64)).to(DEV), k, v, layer=layer,
+                         index=None if index is None else i32(index), stream=stream)
+    torch.cuda.synchronize()
+
+
+def expect(cache, x, dtype, slots, layer=0, index=None):
+    """Bytes of the whole cache and of its factors after the call."""
+    was = [t.cpu().numpy().copy() for t in (cache.k, cache.v, cache.kf, cache.vf)]
+    slots = np.asarray(slots, np.int64)
+    src = np.arange(len(slots)) if index is None else np.asarray(index)
+    good = (slots >= 0) & (slots // cache.block < cache.n_blocks) & (src < x.shape[2])
+    slots, src, layers = slots[good], src[good], slice(layer, layer + x.shape[1])
+    if x.size:
+        for p in range(2):
+            b, f = quantised(x[p], dtype)
+            pad = np.zeros(f.shape[:-1] + (cache.space,), np.uint8)
+            pad[..., :f.shape[-1]] = f
+            was[p][layers, slots // cache.block, slots % cache.block] = b[:, src]
+            was[2 + p][layers, slots // cache.block, slots % cache.block] = pad[:, src]
+    return was
+
+
+def check(cache, want):
+    for name, t, w in zip(("k", "v", "factors of k", "factors of v"), (cache.k, cache.v, cache.kf, cache.vf), want):
+        off = t.cpu().numpy() != w
+        assert not off.any(), f"{name}: {off.sum()} bytes differ, first at {np.argwhere(off)[0]}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("order,parts,heads,block", [("head", 1, 2, 16), ("token", 2, 5, 1), ("token", 1, 3, 8)])
+def test_append(dtype, dim, order, parts, heads, block):
+    cache = QuantCache(heads, dim, block, 9, 3, order, parts)
+    rows = 7
+    x = rows_of(dtype, 2, 2, rows, heads, dim)
+    slots = [4, -1, 9 * block, 0, 9 * block - 1, 2, -(1 << 40)]
+    want = expect(cache, x, dtype, slots, layer=1)
+    append(cache, x, dtype, slots, layer=1)
+    check(cache, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_append_by_index(dtype):
+    cache = QuantCache(2, 128, 16, 4, 2)
+    x = rows_of(dtype, 2, 2, 6, 2, 128)
+    slots, index = [3, 17, 40, 5], [5, 0, 6, 5]  # one row twice, one past the rows
+    want = expect(cache, x, dtype, slots, index=index)
+    append(cache, x, dtype, slots, index=index)
+    check(cache, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_value_of_the_type(dtype):
+    """Every finite number of the 16-bit type in a group whose largest it is, and beside larger ones."""
+    bits = np.arange(65536, dtype=np.uint16).view(np.int16)
+    every = torch.from_numpy(bits.copy()).view(DT[dtype]).double().numpy()
+    every = every[np.isfinite(every)]
+    x = np.zeros((2, 1, len(every), 1, 64))
+    x[0, 0, :, 0, 0] = every
+    x[0, 0, :, 0, 32:] = every[:, None] * np.array([1, 0.5] * 16)
+    x[1, 0, :, 0, :] = every[:, None]
+    x[1, 0, :, 0, 3] = np.minimum(np.abs(every) * 1.7, LARGEST[dtype])
+    x[1, 0, :, 0, 40] = LARGEST[dtype]
+    x = rounded(x, dtype)
+    n = -(-len(every) // 64)
+    cache = QuantCache(1, 64, 64, n)
+    want = expect(cache, x, dtype, range(len(every)))
+    append(cache, x, dtype, range(len(every)))
+    check(cache, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_no_numbers(dtype):
+    """NaN and infinities become NaN and leave the others of their group as they are."""
+    cache = QuantCache(2, 96, 4, 3)
+    x = rows_of(dtype, 2, 1, 8, 2, 96)
+    x[0, 0, 1, 0, 5], x[0, 0, 1, 0, 40], x[0, 0, 2, 1, 95] = np.nan, np.inf, -np.inf
+    x[1, 0, 3, :, 32:64] = np.inf
+    x[1, 0, 4, :, ::2] = -np.nan
+    want = expect(cache, x, dtype, range(8))
+    append(cache, x, dtype, range(8))
+    for t, w in zip((cache.k, cache.v), want):
+        off = t.cpu().numpy() != w
+        off &= ~((w & 127 == NAN) & (t.cpu().numpy() & 127 == NAN))  # a NaN's sign
+        assert not off.any()
+    check(cache, [t.cpu().numpy() for t in (cache.k, cache.v)] + want[2:])
+
+
+def test_strided_rows_and_another_stream():
+    """K and V in one buffer behind the queries, row by row; the call on a stream of its own."""
+    cache = QuantCache(3, 128, 8, 4, 2, "token")
+    x = rows_of("bf16", 2, 2, 9, 3, 128)
+    buffer = torch.zeros(9, 2, 10, 128, dtype=torch.bfloat16, device=DEV)  # rows, layers, heads
+    buffer[:, :, 4:7] = torch.from_numpy(x[0]).to(DEV, torch.bfloat16).transpose(0, 1)
+    buffer[:, :, 7:] = torch.from_numpy(x[1]).to(DEV, torch.bfloat16).transpose(0, 1)
+    slots = [30, 1, 2, 9, 11, 8, 31, 16, 20]
+    want = expect(cache, x, "bf16", slots)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    by_layer = buffer.transpose(0, 1)
+    gift.kv_append_quant(*cache.args(), torch.tensor(slots, device=DEV), by_layer[:, :, 4:7], by_layer[:, :, 7:], stream=s)
+    s.synchronize()
+    check(cache, want)
+
+
+def test_nothing_to_append():
+    cache = QuantCache(1, 64, 16, 2)
+    want = [t.cpu().numpy() for t in (cache.k, cache.v, cache.kf, cache.vf)]
+    append(cache, np.zeros((2, 1, 0, 1, 64)), "bf16", [])
+    append(cache, np.zeros((2, 0, 3, 1, 64)), "bf16", [0, 1, 2])
+    check(cache, want)
+
+
+# --- cached tokens back in 16 bits ---
+
+def read(r, first=None, verdicts=None, rows=None, layers=1, **over):
+    """k and v on the host, 7 where nothing was written; `rows`: of each request."""
+    begin = np.concatenate([[0], np.cumsum(r.lens if rows is None else rows)])
+    out = torch.full((2, layers, int(begin[-1]) + 2, r.cache.heads, r.cache.dim), 7.0, dtype=DT[r.dtype], device=DEV)
+    a = dict(tables=i32(r.tab), lens=i32(r.lens), row_begin=i32(begin))
+    a.update(over)
+    gift.kv_read_quant(*r.cache.args(), a["tables"], a["lens"], a["row_begin"], out[0], out[1], layer=r.layer,
+                       first=None if first is None else i32(first), verdicts=None if verdicts is None else i32(verdicts))
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy(), begin
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,heads,block,order,parts", [(64, 5, 8, "token", 2), (96, 2, 16, "head", 1), (128, 3, 1, "head", 1),
+                                                         (256, 1, 32, "token", 1)])
+def test_read(dtype, dim, heads, block, order, parts):
+    r = Requests([5, 0, 37, 1, 64], [0] * 5, dtype, heads, 1, dim, block, order, parts)
+    got, begin = read(r)
+    assert (got[0, 0, :begin[-1]] == r.k).all() and (got[1, 0, :begin[-1]] == r.v).all()
+    assert (got[:, :, begin[-1]:] == 7).all()
+
+
+def test_read_parts():
+    """From another token on, past the end, more rows than tokens, a refused request, a table entry outside the cache."""
+    r = Requests([40, 20, 33, 9], [0] * 4, "bf16", 2, 1, 128, 8)
+    r.tab[3, 1] = NO_BLOCK
+    rows, first = [10, 30, 20, 9], [35, 0, 0xFFFFFFFF, 0]
+    verdicts = [0, 0, 0, 0]
+    for refused in (None, 1):
+        if refused is not None:
+            verdicts[refused] = gift.SEG_OWNER_MIXED
+        got, begin = read(r, first, verdicts, rows)
+        at = np.concatenate([[0], np.cumsum(r.lens)])
+        want = np.zeros((2, begin[-1], 2, 128))
+        for b in range(4):
+            for i in range(rows[b]):
+                t = first[b] + i
+                if t >= r.lens[b] or verdicts[b] or (b == 3 and t >= 8):
+                    continue
+                want[0, begin[b] + i], want[1, begin[b] + i] = r.k[at[b] + t], r.v[at[b] + t]
+        assert (got[:, 0, :begin[-1]] == want).all()
+
+
+def test_read_rows_of_no_request_stay():
+    r = Requests([4, 6], [0, 0], "bf16", 1, 1, 64, 16)
+    got, _ = read(r, row_begin=i32([2, 4, 10]))
+    assert (got[:, :, :2] == 7).all() and (got[:, :, 10:] == 7).all()
+    assert (got[0, 0, 2:4] == r.k[:2]).all() and (got[1, 0, 4:10] == r.v[4:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_read_every_element_and_factor(dtype):
+    """Every element with the factors that may be written; f16: rounded to the type, past its range infinite."""
+    factors = np.arange(27, 248, dtype=np.uint8)
+    n = len(factors)
+    b = np.tile(np.arange(256, dtype=np.uint8), (n, 1)).reshape(n, 1, 256)
+    f = np.repeat(factors[:, None], 8, 1).reshape(n, 1, 8)
+    cache = QuantCache(1, 256, 1, n)
+    for elements, fs in ((cache.k, cache.kf), (cache.v, cache.vf)):
+        elements[0, :, 0] = torch.from_numpy(b).to(DEV)
+        fs[0, :, 0] = torch.from_numpy(f).to(DEV)
+    out = torch.empty(2, 1, n, 1, 256, dtype=DT[dtype], device=DEV)
+    tables = torch.arange(n, dtype=torch.int32, device=DEV)[None]
+    gift.kv_read_quant(*cache.args(), tables, i32([n]), i32([0, n]), out[0], out[1])
+    got, want = out.double().cpu().numpy()[:, 0], values(b, f, dtype)
+    for x in got:
+        assert (np.isnan(x) == np.isnan(want)).all()
+        assert (x[~np.isnan(want)] == want[~np.isnan(want)]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_back_and_forth(dtype):
+    """What is read back is off by half a step of an element at most, and quantises to the same bytes again."""
+    cache = QuantCache(2, 128, 16, 4)
+    x = rows_of(dtype, 2, 1, 50, 2, 128)
+    append(cache, x, dtype, range(50))
+    out = torch.empty(2, 1, 50, 2, 128, dtype=DT[dtype], device=DEV)
+    args = (torch.arange(4, dtype=torch.int32, device=DEV)[None], i32([50]), i32([0, 50]))
+    gift.kv_read_quant(*cache.args(), *args, out[0], out[1])
+    y = out.double().cpu().numpy()
+    top = np.abs(x.reshape(2, 1, 50, 2, 4, 32)).max(-1, keepdims=True)
+    # elements: 4 bits (half a step 2^-4), or steps of 2^-9 of a factor that is at most 2 / 448 of the largest
+    bound = np.maximum(np.abs(x) * 2.0 ** -4, np.broadcast_to(top * 2.0 ** -10 * 2 / 448, x.shape[:-1] + (4, 32)).reshape(x.shape))
+    assert (np.abs(x - y) <= np.maximum(bound, 2.0 ** -110)).all()
+    before = cache.data.clone()
+    gift.kv_append_quant(*cache.args(), torch.arange(50, device=DEV), out[0], out[1])
+    read_again = torch.empty_like(out)
+    gift.kv_read_quant(*cache.args(), *args, read_again[0], read_again[1])
+    assert torch.equal(out, read_again)
+    assert before.shape == cache.data.shape

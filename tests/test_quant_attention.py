@@ -1,0 +1,216 @@
+"""Attention over a quantised cache against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from kv_helpers import DEV, DT, NO_BLOCK, i32
+from paper_2608_25431_amd import gift
+from quant_helpers import NAN, Requests
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def work():
+    w = gift.AttentionWork()
+    yield w
+    w.destroy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("rows", [[1, 1, 1, 1], [33, 1, 40, 2], [50, 30, 0, 64], [100, 3, 65, 0]])
+@pytest.mark.parametrize("mask", [None, "tree"])
+def test_lengths_and_rows(work, dtype, dim, rows, mask):
+    """Each number of waves that share keys, every type and size of head; lengths that end inside tiles and blocks."""
+    r = Requests(np.array([1, 31, 200, 77]) + rows, rows, dtype, 2, 2, dim, 16, mask=mask)
+    r.check(r.run(work))
+
+
+@pytest.mark.parametrize("block,order,parts,heads,group", [(1, "head", 1, 1, 8), (8, "token", 2, 5, 1), (64, "token", 1, 2, 7),
+                                                           (128, "head", 2, 3, 4)])
+@pytest.mark.parametrize("mask", [None, "holes", "random"])
+def test_layouts(work, block, order, parts, heads, group, mask):
+    rows = [5, 0, 17, 1]
+    r = Requests(np.array([0, 0, 333, 64]) + rows, rows, "bf16", heads, group, 64, block, order, parts, 3, 2, mask)
+    r.check(r.run(work))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("length", [0, 1, 2, 31, 32, 33, 63, 64, 65, 127, 129])
+def test_a_single_row(work, dtype, length):
+    """One token over every length around a tile; of length 0 it sees nothing."""
+    r = Requests([length, length], [1, 1], dtype, 1, 4, 128, 16)
+    r.check(r.run(work))
+
+
+@pytest.mark.parametrize("start", range(0, 40, 3))
+@pytest.mark.parametrize("mask", [None, "random"])
+def test_own_tokens_begin_anywhere_in_a_tile(work, start, mask):
+    r = Requests([start + 41], [41], "bf16", 1, 1, 64, 8, mask=mask, seed=start)
+    r.check(r.run(work))
+
+
+def test_mask_of_fewer_words_than_rows(work):
+    """Rows past 32 * mask_words are not seen."""
+    r = Requests([150], [70], "f16", 2, 2, 64, 16, mask="random")
+    r.bits = r.bits[:, :32]
+    r.check(r.run(work))
+
+
+def test_more_rows_than_tokens(work):
+    """Rows whose own token would be before the first see nothing."""
+    for mask in (None, "random"):
+        r = Requests([5, 0, 40], [9, 3, 40], "bf16", 2, 1, 64, 16, mask=mask)
+        got = r.run(work)
+        r.check(got)
+        if mask is None:
+            assert (got[0][:4] == 0).all() and (got[1][:4] == -np.inf).all()
+
+
+def test_long_contexts_are_split_and_joined(work):
+    for lens, rows in (([40000], [1]), ([9000, 3, 20000], [2, 1, 40])):
+        r = Requests(lens, rows, "bf16", 2, 4, 128, 16, seed=4)
+        r.check(r.run(work))
+
+
+def test_large_scores(work):
+    """Weights of a few keys, far above the others."""
+    for dtype in ("bf16", "f16"):
+        r = Requests([600, 45], [3, 45], dtype, 2, 2, 64, 16, q_scale=30.0)
+        r.check(r.run(work))
+        r.check(r.run(work, scale=-0.3), scale=-0.3)
+        r.check(r.run(work, scale=0.0), scale=0.0)
+
+
+def test_refused_requests_and_rows_of_none(work):
+    r = Requests([50, 60, 70], [2, 40, 5], "bf16", 2, 2, 128, 16)
+    r.verdicts = np.array([0, gift.SEG_OWNER_MIXED, 0])
+    got = r.run(work)
+    r.check(got)
+    assert (got[0][2:42] == 0).all()
+    # two rows before the first request and three behind the last
+    q = r.q
+    r.verdicts = None
+    r.q = torch.cat([q[:2], q, q[:3]])
+    begin, r.begin = r.begin, r.begin + 2
+    got = r.run(work)
+    r.check(got)
+    assert (got[0][:2] == 0).all() and (got[0][-3:] == 0).all() and (got[1][-3:] == -np.inf).all()
+    assert begin[-1] == 47
+
+
+def test_entries_outside_the_cache_are_not_followed(work):
+    r = Requests([100], [3], "bf16", 1, 2, 64, 16)
+    r.tab[0, 2] = NO_BLOCK
+    r.check(r.run(work), unseen=lambda b, j: (j >= 32) & (j < 48))
+
+
+def test_lengths_past_the_table_are_cut(work):
+    r = Requests([64], [2], "bf16", 1, 2, 64, 16)
+    wide = i32(r.tab)[:, :4]
+    r.check(r.run(work, tables=wide, lens=i32([0xFFFFFFFF])))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [[60, 9], [5, 2], [130, 20]])
+@pytest.mark.parametrize("mask", [None, "tree"])
+def test_no_numbers_reach_only_rows_that_see_them(work, dtype, rows, mask):
+    """NaN in V of the rows' own tokens, and of tokens before them."""
+    r = Requests(np.array([20, 33]) + rows, rows, dtype, 2, 2, 64, 16, mask=mask, seed=5)
+    first = np.concatenate([[0], np.cumsum(r.lens)])
+    for b, back, dim in ((0, 1, 3), (0, rows[0] // 2, 40), (1, 1, 63), (1, rows[1] // 2 + 1, 0)):
+        pos = int(r.lens[b]) - back
+        at = (r.layer, int(r.tab[b, pos // 16]), pos % 16, b % 2, dim)
+        r.cache.v[at] = NAN
+        r.v[first[b] + pos, b % 2, dim] = np.nan
+    r.check(r.run(work))
+
+
+def test_no_numbers_in_unseen_keys(work):
+    """A key of the rows' own tokens that is not a number has no part in rows that do not see it."""
+    r = Requests([90], [50], "bf16", 1, 1, 64, 16, seed=6)
+    pos = 89
+    r.cache.k[r.layer, int(r.tab[0, pos // 16]), pos % 16] = NAN
+    out, lse = r.run(work)
+    assert torch.isfinite(out[:49]).all() and torch.isfinite(lse[:49]).all()
+    assert not torch.isfinite(out[49]).any()
+
+
+def test_strides(work):
+    """Queries and outputs head by head."""
+    r = Requests([77, 30], [20, 1], "f16", 2, 3, 64, 16)
+    out = torch.zeros(6, 21, 64, dtype=torch.float16, device=DEV)
+    q = r.q.to(DEV).transpose(0, 1).contiguous()
+    kv = r.cache.args()
+    gift.quant_attention(work, *kv, r.layer, q.transpose(0, 1), i32(r.begin), i32(r.lens), i32(r.tab), out.transpose(0, 1))
+    torch.cuda.synchronize()
+    r.check((out.transpose(0, 1).cpu(), None))
+
+
+def test_the_same_bits_again(work):
+    r = Requests([30000, 5], [3, 5], "bf16", 2, 4, 128, 16)
+    first = r.run(work)
+    for _ in range(5):
+        again = r.run(work)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_a_row_s_bits_do_not_depend_on_those_beside_it(work):
+    """The rows of one request, alone and among others, where the work is cut alike."""
+    r = Requests([64, 64], [4, 4], "bf16", 1, 2, 64, 16)
+    both = r.run(work)
+    r.verdicts = np.array([0, gift.SEG_OWNER_MIXED])
+    assert torch.equal(both[0][:4], r.run(work)[0][:4])
+
+
+def test_streams_and_graphs(work):
+    """Calls on another stream, and two graphs that share a workspace replayed in turn, with eager calls between."""
+    a, b = Requests([500, 40], [1, 1], "bf16", 2, 4, 128, 16, seed=1), Requests([3000], [20], "f16", 2, 2, 64, 16, seed=2)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    a.check(a.run(work, stream=s))
+    graphs, outs = [], []
+    for r in (a, b):
+        q, out = r.q.to(DEV), torch.zeros(r.q.shape, dtype=r.q.dtype, device=DEV)
+        args = (q, i32(r.begin), i32(r.lens), i32(r.tab), out)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            gift.quant_attention(work, *r.cache.args(), r.layer, *args)
+        graphs.append((g, args))
+        outs.append(out)
+    for _ in range(4):
+        for (g, _), out, r in zip(graphs, outs, (a, b)):
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            r.check((out.cpu(), None))
+        a.check(a.run(work))
+
+
+def test_no_requests_and_no_rows(work):
+    r = Requests([20], [3], "bf16", 1, 1, 64, 16)
+    empty = torch.empty(0, 1, 64, dtype=torch.bfloat16, device=DEV)
+    gift.quant_attention(work, *r.cache.args(), 0, empty, i32([0, 0]), i32([20]), i32(r.tab), torch.empty_like(empty))
+    out = torch.ones(3, 1, 64, dtype=torch.bfloat16, device=DEV)
+    gift.quant_attention(work, *r.cache.args(), 0, r.q.to(DEV), i32([0]), i32([]), i32(np.zeros((0, 1))), out)
+    torch.cuda.synchronize()
+    assert (out == 0).all()
+
+
+def test_near_the_unquantised_call(work):
+    """Rows appended to a cache of 16 bits and read by gift_tree_attention give the same outputs as the values of the
+    quantised cache, bit for bit where both see all cached tokens."""
+    from kv_helpers import Cache
+    r = Requests([90, 41], [1, 1], "bf16", 2, 2, 128, 16)
+    cache = Cache("bf16", 2, 128, 16, r.cache.n_blocks, 2)
+    pos, req = r.pos, r.req
+    at = (torch.from_numpy(r.tab[req, pos // 16]).to(DEV), torch.from_numpy(pos % 16).to(DEV))
+    cache.k[r.layer][at] = torch.from_numpy(r.k).to(DEV, torch.bfloat16)
+    cache.v[r.layer][at] = torch.from_numpy(r.v).to(DEV, torch.bfloat16)
+    q, out = r.q.to(DEV), torch.zeros(r.q.shape, dtype=DT["bf16"], device=DEV)
+    gift.tree_attention(work, *cache.args(), r.layer, q, None, None, i32(r.begin), i32(r.lens), i32(r.tab), out)
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), r.run(work)[0])

@@ -1,0 +1,177 @@
+"""The calls around a quantised cache together, as a decode worker makes them: blocks and slots, norm and rotation, rows into
+the cache, attention, and the requests' tokens read back and sealed; eager and replayed."""
+import numpy as np
+import pytest
+import torch
+
+from kv_helpers import DEV, i32
+from paper_2608_25431_amd import gift
+from quant_helpers import HALF_STEP, QuantCache, quantised, values
+
+pytestmark = pytest.mark.gpu
+LAYERS, HEADS, KV_HEADS, DIM, BLOCK, WIDTH, BLOCKS = 2, 8, 2, 64, 8, 12, 40
+USERS = [3, 5, 3]
+
+
+class Worker:
+    def __init__(self, seed=0):
+        self.cache = QuantCache(KV_HEADS, DIM, BLOCK, BLOCKS, LAYERS)
+        n = len(USERS)
+        self.users, self.lens = i32(USERS), i32([0] * n)
+        self.tables = torch.full((n, WIDTH), -1, dtype=torch.int32, device=DEV)
+        self.labels = torch.full((BLOCKS,), -1, dtype=torch.int32, device=DEV)
+        self.free = torch.from_numpy(np.random.default_rng(seed).permutation(BLOCKS).astype(np.int32)).to(DEV)
+        self.work = gift.AttentionWork()
+        self.freq = torch.from_numpy((1e4 ** -(np.arange(DIM // 2) / (DIM // 2))).astype(np.float32)).to(DEV)
+        g = torch.Generator().manual_seed(seed)
+        self.weights = (1 + 0.2 * torch.randn(2, DIM, generator=g)).to(DEV, torch.bfloat16)
+
+    def grow(self, new):
+        n, rows = len(USERS), sum(new)
+        slots = torch.empty(rows, dtype=torch.int64, device=DEV)
+        begin, lens, verdicts, taken = (torch.empty(k, dtype=torch.int32, device=DEV) for k in (n + 1, n, n, 1))
+        gift.kv_tables(self.users, self.lens, i32(new), BLOCK, self.free, self.tables, self.labels, slots, begin, lens, taken,
+                       verdicts)
+        self.free, self.lens = self.free[int(taken):], lens
+        return slots, begin, lens, verdicts
+
+    def layer(self, i, qkv, places, slots, begin, lens, verdicts, out):
+        """One layer: in place in the projection's buffer, into the cache, attention."""
+        q, k, v = qkv.split([HEADS, KV_HEADS, KV_HEADS], 1)
+        gift.qk_norm_rope(q, k, q, k, positions=places, inv_freq=self.freq, q_weight=self.weights[0], k_weight=self.weights[1])
+        gift.kv_append_quant(*self.cache.args(), slots, k[None], v[None], layer=i)
+        gift.quant_attention(self.work, *self.cache.args(), i, q, begin, lens, self.tables, out, verdicts=verdicts)
+
+
+def expect_layer(w, qkv, places, history, new):
+    """Outputs in 64 bits of what the rows' projections give, K and V as their quantised values; appends to history.
+    Keys and queries are rounded before they are used, so that the check starts from the device's own."""
+    out = np.zeros((qkv.shape[0], HEADS, DIM))
+    row = 0
+    for b, count in enumerate(new):
+        x = qkv[row:row + count].double().cpu().numpy()
+        q, k, v = x[:, :HEADS], x[:, HEADS:HEADS + KV_HEADS], x[:, HEADS + KV_HEADS:]
+        for name, y in (("k", k), ("v", v)):
+            history[b][name].append(values(*quantised(y, "bf16"), "bf16"))
+        k, v = (np.concatenate(history[b][name]) for name in ("k", "v"))
+        for i in range(count):
+            seen = len(k) - count + i + 1
+            for h in range(HEADS):
+                s = k[:seen, h // 4] @ q[i, h] * DIM ** -0.5
+                p = np.exp(s - s.max())
+                out[row + i, h] = p @ v[:seen, h // 4] / p.sum()
+        row += count
+    return out
+
+
+def test_prompts_and_steps():
+    w, g = Worker(), torch.Generator().manual_seed(1)
+    history = [[dict(k=[], v=[]) for _ in USERS] for _ in range(LAYERS)]
+    done = [0] * len(USERS)
+    for new in ([19, 1, 40], [1, 1, 1], [3, 0, 2], [1, 1, 1]):
+        slots, begin, lens, verdicts = w.grow(new)
+        assert verdicts.tolist() == [gift.SEG_OK] * len(USERS)
+        places = i32(np.concatenate([done[b] + np.arange(n) for b, n in enumerate(new)]))
+        for i in range(LAYERS):
+            qkv = torch.randn(sum(new), HEADS + 2 * KV_HEADS, DIM, generator=g).to(DEV, torch.bfloat16)
+            out = torch.empty(sum(new), HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+            w.layer(i, qkv, places, slots, begin, lens, verdicts, out)
+            torch.cuda.synchronize()
+            want = expect_layer(w, qkv, places, history[i], new)
+            # scores of a few units, 64 products: far below half a step of the outputs and of V's values, all below 5
+            assert (np.abs(out.double().cpu().numpy() - want) <= HALF_STEP["bf16"] * np.abs(want) + 2.0 ** -13).all()
+        done = [d + n for d, n in zip(done, new)]
+
+    # all tokens back in 16 bits
+    total = sum(done)
+    k, v = torch.empty(2, LAYERS, total, KV_HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+    gift.kv_read_quant(*w.cache.args(), w.tables, w.lens, i32(np.concatenate([[0], np.cumsum(done)])), k, v)
+    for i in range(LAYERS):
+        for got, name in ((k, "k"), (v, "v")):
+            want = np.concatenate([y for h in history[i] for y in h[name]])
+            assert (got[i].double().cpu().numpy() == want).all()
+
+    # the requests leave sealed, elements and factors, and come back into other blocks
+    keys, nonces = np.random.default_rng(2).integers(0, 256, (8, 32), dtype=np.uint8), np.zeros((8, 12), np.uint8)
+    kt, other = gift.KeyTable(keys), QuantCache(KV_HEADS, DIM, BLOCK, BLOCKS, LAYERS)
+    blocks = [w.tables[b, :-(-done[b] // BLOCK)].cpu().numpy().astype(np.uint32) for b in range(len(USERS))]
+    for part, (here, there) in enumerate(zip((w.cache.args()[0], w.cache.args()[2].cache),
+                                             (other.args()[0], other.args()[2].cache))):
+        size = sum(map(len, blocks)) * LAYERS * here.n_parts * here.chunk_bytes
+        sealed, tags = torch.empty(size, dtype=torch.uint8, device=DEV), torch.empty(48, dtype=torch.uint8, device=DEV)
+        ok = torch.empty(3, dtype=torch.int32, device=DEV)
+        seq = [(part * 3 + b) for b in range(3)]
+        gift.seal_paged(here, list(zip(blocks, USERS, seq)), kt, nonces, sealed, tags, block_labels=w.labels, verdicts=ok)
+        assert ok.tolist() == [gift.SEG_OK] * 3
+        gift.open_paged(there, [((x + 7) % BLOCKS, u, s) for x, u, s in zip(blocks, USERS, seq)], kt, nonces, sealed, tags, ok)
+        assert ok.tolist() == [gift.SEG_OK] * 3
+    moved = torch.where(w.tables >= 0, (w.tables + 7) % BLOCKS, w.tables)
+    k2, v2 = torch.empty(2, LAYERS, total, KV_HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+    gift.kv_read_quant(*other.args(), moved, w.lens, i32(np.concatenate([[0], np.cumsum(done)])), k2, v2)
+    assert torch.equal(k, k2) and torch.equal(v, v2)
+    kt.destroy()
+    w.work.destroy()
+
+
+def test_manipulated_table():
+    """A table that names another user's block: no slots, attention of zeros, nothing read back."""
+    w = Worker()
+    slots, begin, lens, verdicts = w.grow([10, 10, 10])
+    x = torch.randn(1, 30, KV_HEADS, DIM, device=DEV).to(torch.bfloat16)
+    for i in range(LAYERS):
+        gift.kv_append_quant(*w.cache.args(), slots, x, x, layer=i)
+    w.tables[1, 0] = w.tables[0, 0]
+    before = w.cache.data.clone()
+    slots, begin, lens, verdicts = w.grow([1, 1, 1])
+    assert verdicts.tolist() == [gift.SEG_OK, gift.SEG_OWNER_MIXED, gift.SEG_OK] and slots[1] == -1
+    gift.kv_append_quant(*w.cache.args(), slots, x[:, :3], x[:, :3])
+    owned = w.tables[1, 1].item()
+    assert torch.equal(before.view(LAYERS, BLOCKS, -1)[:, owned], w.cache.data.view(LAYERS, BLOCKS, -1)[:, owned])
+    q = torch.randn(3, HEADS, DIM, device=DEV).to(torch.bfloat16)
+    out = torch.ones_like(q)
+    gift.quant_attention(w.work, *w.cache.args(), 0, q, begin, lens, w.tables, out, verdicts=verdicts)
+    assert (out[1] == 0).all() and (out[0] != 0).any() and (out[2] != 0).any()
+    k, v = torch.ones(2, LAYERS, 30, KV_HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+    gift.kv_read_quant(*w.cache.args(), w.tables, lens, i32([0, 10, 20, 30]), k, v, verdicts=verdicts)
+    assert (k[:, 10:20] == 0).all() and torch.equal(k[0, :1], k[1, :1])
+    w.work.destroy()
+
+
+def test_a_captured_layer():
+    """A layer of a decode step, captured once and replayed step after step, against the same steps eager."""
+    steps, new = 4, [1, 1, 1]
+    outs = []
+    for captured in (False, True):
+        w, g = Worker(), torch.Generator().manual_seed(3)
+        slots, begin, lens, verdicts = w.grow([20, 3, 9])
+        x = torch.randn(1, 32, KV_HEADS, DIM, generator=g).to(DEV, torch.bfloat16)
+        gift.kv_append_quant(*w.cache.args(), slots, x, x)
+        qkv = torch.zeros(3, HEADS + 2 * KV_HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+        places, out = i32([0, 0, 0]), torch.zeros(3, HEADS, DIM, dtype=torch.bfloat16, device=DEV)
+        kept = [torch.empty_like(t) for t in w.grow(new)]  # where the graph finds slots, rows, lengths and verdicts
+        w.lens = lens
+        graph = None
+        got = []
+        for i in range(steps):
+            for to, t in zip(kept, w.grow(new)):
+                to.copy_(t)
+            qkv.copy_(torch.randn(qkv.shape, generator=g))
+            places.copy_(torch.tensor([20, 3, 9], dtype=torch.int32) + i)
+            if not captured:
+                w.layer(0, qkv, places, *kept, out)
+            elif graph is None:
+                again = qkv.clone()
+                w.layer(0, qkv, places, *kept, out)  # once before the capture
+                qkv.copy_(again)
+                torch.cuda.synchronize()
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    w.layer(0, qkv, places, *kept, out)
+                graph.replay()
+            else:
+                graph.replay()
+            torch.cuda.synchronize()
+            got.append(out.clone())
+        outs.append(torch.stack(got))
+        w.work.destroy()
+    assert torch.equal(*outs) and torch.isfinite(outs[0]).all()
