@@ -115,7 +115,7 @@ template <int D_, int WQ_, int WK_, int TK_, bool QUANT = false>
 struct Shape {
   static constexpr bool kQuant = QUANT;
   typedef typename std::conditional<QUANT, QuantAttnArgs, AttnArgs>::type Args;
-  static constexpr int D = D_, WQ = WQ_, WK = WK_, TK = TK_;
+  static constexpr int D = D_, WQ = WQ_, WK = WK_, TK = TK_, kCols = 32 * WQ;
   static constexpr int kWaves = WQ * WK, kThreads = kWave * kWaves, kTiles = WK * TK;  // per round
   // a wave that shares its tiles with no other needs no second buffer: its LDS accesses are in order
   static constexpr int kBufs = WQ == 1 ? 1 : 2;
@@ -132,6 +132,7 @@ struct Shape {
   static constexpr int kAcc = D / 32;
   static constexpr int kStepTiles = TK >= 2 ? 2 : 1;
   static constexpr bool kQueriesInLds = WQ == 1;
+  static constexpr bool kNeighbours = true;  // workgroups that are neighbours in the order of work run on one XCD
   // 64 requests stay in registers, four a lane; otherwise the next one is loaded when its turn comes, which shows less
   // where a column takes longer
   static constexpr bool kKeepsRequests = WQ == 1 && D <= 128;
@@ -166,7 +167,7 @@ __device__ inline Said said_of(const AttnArgs& p, uint32_t b) {
 // A request as the kernel works on it.
 struct Req {
   uint32_t row0, rows, len, ctx_tiles, tiles, rounds, cols, col_tiles;
-  bool dead;
+  uint32_t dead;
 };
 
 template <class S>
@@ -180,7 +181,7 @@ __device__ inline Req req_of(const AttnArgs& p, const Said& s) {
   r.tiles = r.ctx_tiles + (p.a.k ? (r.rows + kTileKeys - 1) / kTileKeys : 0);
   const uint32_t rounds = (r.tiles + S::kTiles - 1) / S::kTiles;
   r.rounds = r.dead || rounds == 0 ? 1 : rounds;
-  r.col_tiles = (uint32_t)(((uint64_t)r.rows * p.group + 32 * S::WQ - 1) / (32 * S::WQ));
+  r.col_tiles = (uint32_t)(((uint64_t)r.rows * p.group + S::kCols - 1) / S::kCols);
   r.cols = r.col_tiles * p.kv.heads;
   return r;
 }
@@ -265,35 +266,22 @@ __device__ inline float max_of_halves(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Work is cut evenly: a round (kTiles tiles of 32 keys) of a column tile (32 WQ
-// rows of one request and KV head) is a unit, and of all units in a row every
-// workgroup takes the same number, whichever requests they belong to.  A column
-// whose units lie in several workgroups is joined by the one that finishes last,
-// in the order of the parts, so that the result does not depend on who that is.
-// Bound by memory where rows are few: K and V of 131072 tokens (8 heads of 128
-// elements, 537 MB) take 111 us, 4.8 TB/s, which is what a large copy reaches.
-// With many rows by what a wave does one after the other: 32 requests of
-// 2048-8192 tokens with trees of 16-32 tokens and 64 heads (729 MB, 142 GFLOP)
-// take 290 us.  Without products and exponentials the loads and stores alone take
-// 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
-// two waves a SIMD that meet once a round hide a third of that.
-template <class E, class S, int MINW>
-__global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S::Args p, uint8_t* work) {
-  typedef typename E::vec vec;
-  const gift_tree_attention_args& a = p.a;
-  __shared__ __align__(16) uint8_t area[S::kArea];
-  __shared__ __align__(16) uint8_t queries[S::kQueriesInLds ? 32 * S::kKRow : 16];
-  __shared__ uint8_t row_flags[S::kBufs][S::kTiles][kTileKeys];  // bit 0: the key exists, bit 1: its V is not finite
-  __shared__ uint64_t sums[S::kWaves];
-  __shared__ uint64_t found[2];
-  __shared__ uint32_t last_one;
-  const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave),
-                 wq = wave % S::WQ, wk = wave / S::WQ, half = lane / 32, col = lane % 32;
-  uint32_t n_wg = gridDim.x, wg = blockIdx.x;
+// A workgroup's share of the work: units first .. end - 1 of all in a row, the first of them in request b0 + bi, whose own
+// first one is base.
+struct Cut {
+  uint32_t n_wg, wg;  // workgroups that have a share, and which of them this is
+  uint32_t b0, bi;
+  uint64_t total, first, end, base;
+  Said said;  // of requests b0 + lane
+};
 
-  // This workgroup's units, and the request that holds the first of them.  Every workgroup sums the requests' units
-  // itself: up to 64 of them each wave for itself, a request a lane, without waiting for another; more of them the
-  // workgroup together.
+// Every workgroup sums the requests' units itself: up to 64 of them each wave for itself, a request a lane, without waiting
+// for another; more of them the workgroup together.  False: nothing to do.  Rows of no request are seen to on the way.
+template <class S, class Args>
+__device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t wave, uint32_t lane, uint64_t* sums,
+                                         uint64_t* found, Cut& x) {
+  const gift_tree_attention_args& a = p.a;
+  uint32_t n_wg = x.n_wg, wg = x.wg;
   const uint32_t row_first = a.n_reqs ? a.row_begin[0] : 0, row_last = a.n_reqs ? a.row_begin[a.n_reqs] : 0;
   Said said{0, 0, 0, 0};  // of requests b0 + lane
   if (a.n_reqs) said = said_of(p, lane);
@@ -313,14 +301,14 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
         for (uint32_t h = tid; h < a.n_heads; h += S::kThreads) a.lse[(uint64_t)r * a.n_heads + h] = -INFINITY;
     }
   }
-  if (a.n_reqs == 0) return;
-  uint32_t b0 = 0, bi = 0;       // bi: the current request among them
-  uint64_t total, unit, unit_end, base;  // base: first unit of the current request
+  if (a.n_reqs == 0) return false;
+  uint32_t b0 = 0, bi = 0;
+  uint64_t total, unit, base;
   auto share = [&]() -> bool {
     if (total < n_wg) {
       if (wg >= total) return false;
       n_wg = (uint32_t)total;  // a unit each
-    } else if (n_wg % 8 == 0) {
+    } else if (S::kNeighbours && n_wg % 8 == 0) {
       // neighbours in the order of work share an XCD (and its L2), where column tiles of one KV head read the same keys
       wg = wg % 8 * (n_wg / 8) + wg / 8;
     }
@@ -350,7 +338,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
   if (a.n_reqs <= kWave) {
     const uint64_t mine = units_of<S>(p, said), upto = running(mine);
     total = uniform(__shfl((unsigned long long)upto, kWave - 1));
-    if (!share()) return;
+    if (!share()) return false;
     unit = first_of(wg);
     bi = __builtin_ctzll(__ballot(unit < upto));
     base = uniform(__shfl((unsigned long long)(upto - mine), bi));
@@ -369,7 +357,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
       total += sums[w];
     }
     total = uniform(total);
-    if (!share()) return;
+    if (!share()) return false;
     unit = first_of(wg);
     if (upto - mine <= unit && unit < upto) {
       uint64_t at = upto - mine;
@@ -387,11 +375,54 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
     base = uniform(found[1]);
     said = said_of(p, b0 + lane);
   }
+  x.n_wg = n_wg;
+  x.wg = wg;
+  x.b0 = b0;
+  x.bi = bi;
+  x.total = total;
+  x.base = base;
+  x.said = said;
   // scalar from here on: divisions leave vector registers
-  unit = uniform(unit);
-  unit_end = uniform(first_of(wg + 1));
-  const uint64_t first = unit;
+  x.first = uniform(unit);
+  x.end = uniform(first_of(wg + 1));
+  return true;
+}
 
+// Work is cut evenly: a round (kTiles tiles of 32 keys) of a column tile (32 WQ
+// rows of one request and KV head) is a unit, and of all units in a row every
+// workgroup takes the same number, whichever requests they belong to.  A column
+// whose units lie in several workgroups is joined by the one that finishes last,
+// in the order of the parts, so that the result does not depend on who that is.
+// Bound by memory where rows are few: K and V of 131072 tokens (8 heads of 128
+// elements, 537 MB) take 111 us, 4.8 TB/s, which is what a large copy reaches.
+// With many rows by what a wave does one after the other: 32 requests of
+// 2048-8192 tokens with trees of 16-32 tokens and 64 heads (729 MB, 142 GFLOP)
+// take 290 us.  Without products and exponentials the loads and stores alone take
+// 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
+// two waves a SIMD that meet once a round hide a third of that.
+template <class E, class S, int MINW>
+__global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S::Args p, uint8_t* work) {
+  typedef typename E::vec vec;
+  const gift_tree_attention_args& a = p.a;
+  __shared__ __align__(16) uint8_t area[S::kArea];
+  __shared__ __align__(16) uint8_t queries[S::kQueriesInLds ? 32 * S::kKRow : 16];
+  __shared__ uint8_t row_flags[S::kBufs][S::kTiles][kTileKeys];  // bit 0: the key exists, bit 1: its V is not finite
+  __shared__ uint64_t sums[S::kWaves];
+  __shared__ uint64_t found[2];
+  __shared__ uint32_t last_one;
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave),
+                 wq = wave % S::WQ, wk = wave / S::WQ, half = lane / 32, col = lane % 32;
+
+  // this workgroup's units, and the request that holds the first of them
+  Cut cut;
+  cut.n_wg = gridDim.x;
+  cut.wg = blockIdx.x;
+  if (!cut_work<S>(p, tid, wave, lane, sums, found, cut)) return;
+  const uint32_t n_wg = cut.n_wg, wg = cut.wg;
+  uint32_t b0 = cut.b0, bi = cut.bi;  // bi: the current request among those of said
+  Said said = cut.said;               // of requests b0 + lane
+  const uint64_t total = cut.total, first = cut.first, unit_end = cut.end;
+  uint64_t unit = first, base = cut.base;  // base: first unit of the current request
   const float c = fmaxf(fabsf(a.scale) * 1.44269504f, 1.17549435e-38f);
   const uint32_t neg = a.scale < 0 ? 0x80008000u : 0u;
   const uint32_t row_lane = lane % S::kRows;  // the row whose address this lane works out

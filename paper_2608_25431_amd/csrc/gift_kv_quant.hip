@@ -5,6 +5,7 @@
 
 #include "gift_kv_attention.hpp"
 #include "gift_kv_internal.hpp"
+#include "gift_kv_narrow.hpp"
 
 namespace gift {
 namespace {
@@ -308,6 +309,29 @@ hipError_t norm_rope(const gift_qk_rows& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// With 256 elements a wave takes all registers of its SIMD.
+template <class E, int W>
+hipError_t attend_rows_by_dim(const QuantAttnArgs& a, const AttnWork& w, hipStream_t s) {
+  switch (a.kv.head_dim) {
+    case 64: return attend_rows<E, Narrow<64, W>, 2>(a, w, s);
+    case 96: return attend_rows<E, Narrow<96, W>, 2>(a, w, s);
+    case 128: return attend_rows<E, Narrow<128, W>, 2>(a, w, s);
+    default: return attend_rows<E, Narrow<256, 4>, 1>(a, w, s);
+  }
+}
+
+// Up to 16 rows at a KV head on average the tiles are 16 columns wide (64 single tokens over 128-2048: 62 us with 32, 49
+// with 16).  Two workgroups of four waves a CU, so that one's loads fill the other's changes of columns (49 us, with one of
+// eight 64); where there are no more columns than CUs, one of eight, whose columns have fewer parts to join (one request of
+// 8192 tokens: 20.7 with four, 17.8; of 131072 the same).
+template <class E>
+hipError_t attend_quantised(const QuantAttnArgs& a, const AttnWork& w, hipStream_t s) {
+  const uint64_t rows = a.a.n_reqs ? (a.a.n_rows * a.group + a.a.n_reqs - 1) / a.a.n_reqs : 1;
+  if (rows <= 16)
+    return (uint64_t)a.a.n_reqs * a.kv.heads <= w.cus ? attend_rows_by_dim<E, 8>(a, w, s) : attend_rows_by_dim<E, 4>(a, w, s);
+  return attend_by_dim<E>(a, w, s);
+}
+
 }  // namespace
 
 hipError_t launch_qk_norm_rope(const gift_qk_rows& a, hipStream_t s) {
@@ -335,7 +359,7 @@ hipError_t launch_kv_read_quant(const QuantReadArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s) {
-  return dtype == GIFT_BF16 ? attend_by_dim<Bf16Quant>(a, w, s) : attend_by_dim<F16>(a, w, s);
+  return dtype == GIFT_BF16 ? attend_quantised<Bf16Quant>(a, w, s) : attend_quantised<F16>(a, w, s);
 }
 
 }  // namespace gift

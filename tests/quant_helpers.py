@@ -162,13 +162,13 @@ class Requests:
         """(out, lse, bound on out, bound on lse) in 64 bits.
 
         K and V are exact.  Scores are sums of dim products in 32 bits, off by e <= (dim + 8) 2^-24 sum |q k| scale, and
-        their exponentials by 2^-20 and 2^-22 of the score more.  A weight is rounded to the type (bfloat16: to 16 bits, in
-        two parts), the output once.  With u half a step and w the weight's,
-            |out - exact| <= u |out| + (w + 2 e) sum p |v|
+        their exponentials by 2^-20 and 2^-22 of the score more.  A weight is rounded to the type once (the sum of the weights
+        is of unrounded ones), and so is the output.  With u half a step of the type,
+            |out - exact| <= u |out| + (u + 2 e) sum p |v|
         and f16 weights below 2^-29 of the largest are off by 2^-39 of it, which is less than LEAST for each key."""
         q = self.q.double().numpy()
         h, g, dim = self.cache.heads, self.group, self.cache.dim
-        u, w = HALF_STEP[self.dtype], 2.0 ** -15 if self.dtype == "bf16" else 2.0 ** -11
+        u = HALF_STEP[self.dtype]
         scale = dim ** -0.5 if scale is None else scale
         out, lse = np.zeros(q.shape), np.full(q.shape[:2], -np.inf)
         tol, ltol = np.zeros(q.shape), np.zeros(q.shape[:2])
@@ -196,7 +196,7 @@ class Requests:
                     out[lo + i, j], lse[lo + i, j] = o, m + np.log(total)
                     e = (dim + 8) * 2.0 ** -24 * (np.abs(kk[some]) @ np.abs(q[lo + i, j])).max() * abs(scale)
                     e += 2.0 ** -22 * np.abs(s).max() + 2.0 ** -20
-                    tol[lo + i, j] = u * np.abs(o) + (w + 2 * e) * size + LEAST[self.dtype] * (len(some) + 1)
+                    tol[lo + i, j] = u * np.abs(o) + (u + 2 * e) * size + LEAST[self.dtype] * (len(some) + 1)
                     ltol[lo + i, j] = e + 2.0 ** -22 * abs(lse[lo + i, j])
         return out, lse, tol, ltol
 
