@@ -534,6 +534,15 @@ def _rows_of(x, fmt, want, name):
 
 def _rows_like(x, code, want, name):
     """As _rows_of, of a type by its code."""
+    try:  # the usual tensor, without a look at each of its properties by name
+        if x.is_cuda and _codes[x.dtype] == code and x.shape == want:
+            strides = x.stride()
+            if strides[-1] == 1:
+                if 1 in want:
+                    return x.data_ptr(), [s + s if n > 1 else 0 for n, s in zip(want, strides[:-1])]
+                return x.data_ptr(), [s + s for s in strides[:-1]]
+    except (AttributeError, KeyError, TypeError):
+        pass
     if not getattr(x, "is_cuda", False):
         raise ValueError(f"{name}: tensor must be on the GPU")
     if _code(x.dtype) != code:
@@ -547,6 +556,17 @@ def _code16(x, name):
     if code != BF16 and code != F16:
         raise ValueError(f"{name}: needs a tensor of bfloat16 or float16")
     return code
+
+
+def _weight(w, code, dim, name):
+    """Address of a norm's weights, 0 for None."""
+    if w is None:
+        return 0
+    if _code16(w, name) != code:
+        raise ValueError(f"{name}: {w.dtype} is not the rows' type")
+    if w.numel() != dim:
+        raise ValueError(f"{name}: {w.numel()} elements, the call needs {dim}")
+    return _dev(w, 2 * dim, name)
 
 
 def _strided(x, want, name):
@@ -736,37 +756,35 @@ def qk_norm_rope(q, k, q_out, k_out, positions=None, inv_freq=None, q_weight=Non
         kv_heads = k.shape[1] if len(k.shape) == 3 else 0
         kp, ks = _rows_like(k, code, (rows, kv_heads, dim), "k")
         ko, kos = _rows_like(k_out, code, (rows, kv_heads, dim), "k_out")
-    weights = []
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            if _code16(w, name) != code:
-                raise ValueError(f"{name}: {w.dtype} is not the rows' type")
-            if w.numel() != dim:
-                raise ValueError(f"{name}: {w.numel()} elements, the call needs {dim}")
-            w = _dev(w, 2 * dim, name)
-        weights.append(w or 0)
-    turned = places = freq = stride = 0
+    places = freq = pairs = stride = 0
     axes, parts = 1, (0, 0, 0, 0)
     if inv_freq is not None:
-        turned = 2 * inv_freq.numel()
-        freq = _floats(inv_freq, "inv_freq")
+        freq, pairs = _floats(inv_freq, "inv_freq"), inv_freq.numel()
         if positions is None:
             raise ValueError("positions: needed with inv_freq")
-        axes = positions.shape[0] if len(positions.shape) == 2 else 1
-        if len(positions.shape) not in (1, 2) or positions.shape[-1] < rows or not 1 <= axes <= 4:
-            raise ValueError(f"positions: shape {tuple(positions.shape)}, the call needs {rows} a row, of 1 to 4 axes")
-        if not positions.is_cuda or positions.element_size() != 4 or positions.dtype.is_floating_point or \
-                (positions.shape[-1] > 1 and positions.stride(-1) != 1):
-            raise ValueError("positions: needs adjacent int32 on the GPU")
-        stride = positions.stride(0) if axes > 1 else positions.shape[-1]
-        places = positions.data_ptr()
-        parts = [inv_freq.numel()] if sections is None and axes == 1 else list(sections or ())
-        if len(parts) != axes or min(parts) < 0:
-            raise ValueError(f"sections: needs the pairs of {axes} axes")
-        parts += [0] * (4 - axes)
-    a = _QK.pack(rows, heads, kv_heads, dim, code, qp, kp, qo, ko, *qs, *ks, *qos, *kos, *weights, eps, turned,
-                 int(bool(interleaved)), axes, *parts, freq, places, stride)
+        places, axes, stride = _positions(positions, rows)
+        if sections is None and axes == 1:
+            parts = (pairs, 0, 0, 0)
+        else:
+            parts = [*(sections or ()), 0, 0, 0][:4]
+            if len(sections or ()) != axes or min(parts) < 0:
+                raise ValueError(f"sections: needs the pairs of {axes} axes")
+    a = _QK.pack(rows, heads, kv_heads, dim, code, qp, kp, qo, ko, *qs, *ks, *qos, *kos,
+                 _weight(q_weight, code, dim, "q_weight"), _weight(k_weight, code, dim, "k_weight"), eps, 2 * pairs,
+                 1 if interleaved else 0, axes, *parts, freq, places, stride)
     _check(lib().gift_qk_norm_rope(a, _stream(stream)))
+
+
+def _positions(x, rows):
+    """Address, axes and stride (in entries) of int32 positions, [rows] or [axes][rows]."""
+    shape = x.shape
+    if len(shape) not in (1, 2) or shape[-1] < rows or (len(shape) == 2 and not 1 <= shape[0] <= 4):
+        raise ValueError(f"positions: shape {tuple(shape)}, the call needs {rows} a row, of 1 to 4 axes")
+    strides = x.stride()
+    if not x.is_cuda or x.element_size() != 4 or x.dtype.is_floating_point or (strides[-1] != 1 and shape[-1] > 1):
+        raise ValueError("positions: needs adjacent int32 on the GPU")
+    axes = shape[0] if len(shape) == 2 else 1
+    return x.data_ptr(), axes, strides[0] if axes > 1 else shape[-1]
 
 
 def _floats(x, name):
