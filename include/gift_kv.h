@@ -265,7 +265,8 @@ typedef struct {
  *     y = x * weight / sqrt(mean(x^2) + eps)          (where there is a weight)
  *     (a, b) -> (a cos t - b sin t, b cos t + a sin t) of each pair i of y,
  *     t = positions[axis of i][row] * inv_freq[i]
- * All in 32-bit floats, rounded once at the end; the number of turns of an
+ * All in 32-bit floats, rounded once at the end (where the squares of a head
+ * pass their range, its norm is taken as infinite); the number of turns of an
  * angle is taken in 64 bits, so that far positions keep theirs.
  * Outputs overlap nothing else that the call uses (GIFT_E_INVALID), except
  * that q_out may be q and k_out may be k; queries and keys may lie in one
@@ -305,7 +306,8 @@ typedef struct {
  * ties to even.  What would be past the range of the rows' type when read back
  * becomes the largest element that is not (240 times the factor); NaN and
  * infinities become NaN (0x7F with the sign).  The bytes of a row of factors
- * past head_dim / 32 become 0.
+ * past head_dim / 32 become 0.  What a slot that appears twice holds is not
+ * defined.
  * Errors: as gift_kv_append, and GIFT_E_INVALID for layers past the cache's.
  */
 gift_status gift_kv_append_quant(const gift_paged_kv* kv, const gift_kv_format* format, const gift_kv_scales* scales,

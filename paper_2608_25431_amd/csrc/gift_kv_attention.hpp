@@ -133,6 +133,7 @@ struct Shape {
   static constexpr int kStepTiles = TK >= 2 ? 2 : 1;
   static constexpr bool kQueriesInLds = WQ == 1;
   static constexpr bool kNeighbours = true;  // workgroups that are neighbours in the order of work run on one XCD
+  static constexpr uint32_t kWhole = QUANT ? 20 : 0;  // tiles of columns that need not be divided
   // 64 requests stay in registers, four a lane; otherwise the next one is loaded when its turn comes, which shows less
   // where a column takes longer
   static constexpr bool kKeepsRequests = WQ == 1 && D <= 128;
@@ -186,10 +187,17 @@ __device__ inline Req req_of(const AttnArgs& p, const Said& s) {
   return r;
 }
 
+// Units of a request's columns: rounds, or whole columns.
 template <class S>
-__device__ inline uint64_t units_of(const AttnArgs& p, const Said& s) {
+__device__ inline uint64_t units_of(const AttnArgs& p, const Said& s, bool whole) {
   const Req r = req_of<S>(p, s);
-  return (uint64_t)r.cols * r.rounds;
+  return whole ? r.cols : (uint64_t)r.cols * r.rounds;
+}
+// Columns of a request, from 2^32 on where one of them has more tiles than kWhole.
+template <class S>
+__device__ inline uint64_t columns_of(const AttnArgs& p, const Said& s) {
+  const Req r = req_of<S>(p, s);
+  return r.cols | (r.cols && r.tiles > S::kWhole ? 1ull << 32 : 0);
 }
 
 // Request b0 + i in scalar registers, of the 64 that a wave's lanes hold.
@@ -272,7 +280,9 @@ struct Cut {
   uint32_t n_wg, wg;  // workgroups that have a share, and which of them this is
   uint32_t b0, bi;
   uint64_t total, first, end, base;
-  Said said;  // of requests b0 + lane
+  Said said;       // of requests b0 + lane
+  uint32_t whole;  // units are whole columns
+  __device__ uint32_t units(const Req& r) const { return whole ? 1 : r.rounds; }  // of a column
 };
 
 // Every workgroup sums the requests' units itself: up to 64 of them each wave for itself, a request a lane, without waiting
@@ -304,6 +314,7 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
   if (a.n_reqs == 0) return false;
   uint32_t b0 = 0, bi = 0;
   uint64_t total, unit, base;
+  bool whole = false;
   auto share = [&]() -> bool {
     if (total < n_wg) {
       if (wg >= total) return false;
@@ -332,11 +343,17 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
     }
     return v;
   };
+  // Columns that are not long stay whole where no workgroup has more than one and there are enough of them: what joining
+  // costs is then more than what an even cut gives.  In us, over a quantised cache: 64 single tokens over 32-256 cached ones
+  // cut evenly 24, whole 13, over 100-500 26 and 18; 16 requests of 1-16 rows over up to 500 29 and 19; one token over 512
+  // 12 and 14; where columns have up to 64 tiles, 64 over 128-2048 49 and 56.
+  auto few = [&](uint64_t columns) -> bool { return columns <= n_wg && columns > 128; };
   auto first_of = [&](uint32_t w) -> uint64_t {
     return n_wg == total ? w : quotient(w * total, n_wg, 1.0 / (double)n_wg);
   };
   if (a.n_reqs <= kWave) {
-    const uint64_t mine = units_of<S>(p, said), upto = running(mine);
+    if constexpr (S::kWhole > 0) whole = few(uniform(__shfl((unsigned long long)running(columns_of<S>(p, said)), kWave - 1)));
+    const uint64_t mine = units_of<S>(p, said, whole), upto = running(mine);
     total = uniform(__shfl((unsigned long long)upto, kWave - 1));
     if (!share()) return false;
     unit = first_of(wg);
@@ -345,8 +362,20 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
   } else {
     const uint32_t per = (a.n_reqs + S::kThreads - 1) / S::kThreads;
     uint64_t mine = 0;
+    if constexpr (S::kWhole > 0) {
+      uint64_t own = 0, all = 0;
 #pragma unroll 4
-    for (uint32_t i = 0; i < per; i++) mine += units_of<S>(p, said_of(p, tid * per + i));
+      for (uint32_t i = 0; i < per; i++) own += columns_of<S>(p, said_of(p, tid * per + i));
+      own = running(own);
+      if (lane == kWave - 1) sums[wave] = own;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < S::kWaves; w++) all += sums[w];
+      __syncthreads();
+      whole = few(uniform(all));
+    }
+#pragma unroll 4
+    for (uint32_t i = 0; i < per; i++) mine += units_of<S>(p, said_of(p, tid * per + i), whole);
     uint64_t upto = running(mine);
     if (lane == kWave - 1) sums[wave] = upto;
     __syncthreads();
@@ -363,7 +392,7 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
       uint64_t at = upto - mine;
       uint32_t b = tid * per;
       for (;; b++) {
-        const uint64_t n = units_of<S>(p, said_of(p, b));
+        const uint64_t n = units_of<S>(p, said_of(p, b), whole);
         if (unit < at + n) break;
         at += n;
       }
@@ -382,6 +411,7 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
   x.total = total;
   x.base = base;
   x.said = said;
+  x.whole = whole;
   // scalar from here on: divisions leave vector registers
   x.first = uniform(unit);
   x.end = uniform(first_of(wg + 1));
@@ -440,8 +470,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
 
   Req r = req_at<S>(p, said, bi);
   while (unit < unit_end) {
-    while (unit >= base + (uint64_t)r.cols * r.rounds) {
-      base += (uint64_t)r.cols * r.rounds;
+    while (unit >= base + (uint64_t)r.cols * cut.units(r)) {
+      base += (uint64_t)r.cols * cut.units(r);
       if (++bi == kWave || !S::kKeepsRequests) {
         b0 += bi;
         bi = 0;
@@ -449,10 +479,10 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
       }
       r = req_at<S>(p, said, bi);
     }
-    const Unit at = unit_of(unit - base, r.rounds);
+    const Unit at = unit_of(unit - base, cut.units(r));
     const uint32_t column = __builtin_amdgcn_readfirstlane(at.column), it0 = __builtin_amdgcn_readfirstlane(at.round);
-    const uint64_t col_first = unit - it0, col_last = col_first + r.rounds - 1;
-    const uint32_t it1 = (uint32_t)(unit_end - unit < r.rounds - it0 ? it0 + (unit_end - unit) : r.rounds);
+    const uint64_t col_first = unit - it0, col_last = col_first + cut.units(r) - 1;
+    const uint32_t it1 = !cut.whole && unit_end - unit < r.rounds - it0 ? (uint32_t)(it0 + (unit_end - unit)) : r.rounds;
     const uint32_t g = __builtin_amdgcn_readfirstlane(quotient(column, r.col_tiles)), ct = column - g * r.col_tiles;
     // this lane's query row
     const uint32_t rows = r.rows * p.group, qrow = (ct * S::WQ + wq) * 32 + col;
@@ -1061,7 +1091,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
       }
     }
     __syncthreads();
-    unit += it1 - it0;
+    unit += cut.whole ? 1 : it1 - it0;
   }
 }
 

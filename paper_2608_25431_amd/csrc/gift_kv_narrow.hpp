@@ -31,6 +31,7 @@ struct Narrow {
   typedef QuantAttnArgs Args;
   static constexpr int D = D_, kCols = 16, kWaves = W_, kThreads = kWave * kWaves, kTiles = kWaves, kPieces = D / 8;
   static constexpr bool kNeighbours = false;
+  static constexpr uint32_t kWhole = 20;
   static constexpr int kSteps = D / 32;                       // of 32 elements of a score's product
   static constexpr int kFull = D / 64, kHalf = D / 32 % 2;    // loads of 16 bytes and of 8 that a lane makes of a row
   static constexpr int kWords = D == 256 ? 2 : 1;             // of a row's factors
@@ -89,8 +90,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
   auto describe = [&](uint64_t unit) -> Column {
     Column x;
     x.r = req_at<S>(p, said, bi);
-    while (unit >= base + (uint64_t)x.r.cols * x.r.rounds) {
-      base += (uint64_t)x.r.cols * x.r.rounds;
+    while (unit >= base + (uint64_t)x.r.cols * cut.units(x.r)) {
+      base += (uint64_t)x.r.cols * cut.units(x.r);
       if (++bi == kWave) {
         b0 += bi;
         bi = 0;
@@ -98,11 +99,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
       }
       x.r = req_at<S>(p, said, bi);
     }
-    const Unit at = unit_of(unit - base, x.r.rounds);
+    const Unit at = unit_of(unit - base, cut.units(x.r));
     const uint32_t column = __builtin_amdgcn_readfirstlane(at.column);
     x.b = b0 + bi;
     x.it0 = __builtin_amdgcn_readfirstlane(at.round);
-    x.it1 = (uint32_t)(unit_end - unit < x.r.rounds - x.it0 ? x.it0 + (unit_end - unit) : x.r.rounds);
+    x.it1 = !cut.whole && unit_end - unit < x.r.rounds - x.it0 ? (uint32_t)(x.it0 + (unit_end - unit)) : x.r.rounds;
     x.g = __builtin_amdgcn_readfirstlane(quotient(column, x.r.col_tiles));
     x.ct = column - x.g * x.r.col_tiles;
     x.live = !x.r.dead && x.r.tiles;
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
       return x;
     };
     const uint64_t col_first = unit - now.it0;
-    const uint32_t w0 = owner(col_first), parts = owner(col_first + r.rounds - 1) - w0 + 1;
+    const uint32_t w0 = owner(col_first), parts = owner(col_first + cut.units(r) - 1) - w0 + 1;
     if (qu.live)
 #pragma unroll 1
       for (int t = wave; t < S::kAcc; t += S::kWaves)
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
       }
     }
     __syncthreads();
-    unit += now.it1 - now.it0;
+    unit += cut.whole ? 1 : now.it1 - now.it0;
   }
 }
 

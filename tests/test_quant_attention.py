@@ -74,6 +74,37 @@ def test_long_contexts_are_split_and_joined(work):
         r.check(r.run(work))
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("most", [1, 9, 40])
+@pytest.mark.parametrize("longest", [300, 700])
+def test_many_requests(work, dtype, dim, most, longest):
+    """More requests than a wave has lanes, some without rows or tokens; columns that stay whole, and that are divided where
+    one of them is long."""
+    r = np.random.default_rng(most)
+    rows = r.integers(0 if most > 1 else 1, most + 1, 90)
+    lens = r.integers(0, 300, 90)
+    lens[17] = longest
+    q = Requests(lens + rows, rows, dtype, 3, 1, dim, 16, mask="holes" if most > 1 else None, seed=most)
+    q.verdicts = (r.random(90) < 0.05) * gift.SEG_OWNER_MIXED
+    q.check(q.run(work))
+
+
+@pytest.mark.parametrize("group", [1, 3, 16, 17])
+@pytest.mark.parametrize("heads", [1, 5])
+def test_query_heads_of_a_kv_head(work, group, heads):
+    """Single tokens with as many rows at a KV head as a tile has columns, and one more."""
+    r = Requests([70, 1, 130], [1, 1, 1], "bf16", heads, group, 64, 16)
+    r.check(r.run(work))
+
+
+@pytest.mark.parametrize("rows", [[1] * 40, [17, 2, 30] + [1] * 37])
+def test_columns_of_many_parts_and_whole_ones(work, rows):
+    """Few long requests beside many short ones: some columns are joined from many workgroups, others lie within one."""
+    lens = np.array([6000, 4, 2500] + [20] * 37)
+    r = Requests(lens + rows, rows, "f16", 2, 2, 64, 32, order="token", seed=9)
+    r.check(r.run(work))
+
+
 def test_large_scores(work):
     """Weights of a few keys, far above the others."""
     for dtype in ("bf16", "f16"):
@@ -113,13 +144,13 @@ def test_lengths_past_the_table_are_cut(work):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("rows", [[60, 9], [5, 2], [130, 20]])
+@pytest.mark.parametrize("rows", [[60, 9], [5, 2], [130, 20], [1, 4]])
 @pytest.mark.parametrize("mask", [None, "tree"])
 def test_no_numbers_reach_only_rows_that_see_them(work, dtype, rows, mask):
     """NaN in V of the rows' own tokens, and of tokens before them."""
     r = Requests(np.array([20, 33]) + rows, rows, dtype, 2, 2, 64, 16, mask=mask, seed=5)
     first = np.concatenate([[0], np.cumsum(r.lens)])
-    for b, back, dim in ((0, 1, 3), (0, rows[0] // 2, 40), (1, 1, 63), (1, rows[1] // 2 + 1, 0)):
+    for b, back, dim in ((0, 1, 3), (0, max(1, rows[0] // 2), 40), (1, 1, 63), (1, rows[1] // 2 + 1, 0)):
         pos = int(r.lens[b]) - back
         at = (r.layer, int(r.tab[b, pos // 16]), pos % 16, b % 2, dim)
         r.cache.v[at] = NAN
