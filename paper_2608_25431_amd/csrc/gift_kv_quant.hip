@@ -49,7 +49,9 @@ constexpr int kMostPairs = 128;
 // other (or each within itself, where pairs are adjacent), so that a rotation
 // needs no other lane; a head's sum of squares is joined over its 4 to 16
 // lanes.  The rows' sines and cosines are worked out once a workgroup, of
-// angles whose whole turns are taken off in 64 bits.
+// angles whose whole turns are taken off in 64 bits.  Bound by memory: 17203
+// rows of 40 heads of 128 elements (352 MB read and written) take 72 us, 4.9
+// TB/s, which is what a large copy reaches; one row 2.9, a launch about 2.
 template <class E, int D>
 __global__ __launch_bounds__(kThreads) void k_qk_norm_rope(gift_qk_rows a, uint32_t rows_each) {
   constexpr int kUsed = D / 16, kGroup = kUsed <= 4 ? 4 : kUsed <= 8 ? 8 : 16;  // lanes of a head
@@ -194,7 +196,9 @@ __device__ inline uint32_t quantise(const u32x4 (&x)[2], u32x4& y) {
 
 // A thread quantises 16 elements of K and of V of one row; rows, heads and
 // pieces in the order in which the sources have them, layers along the grid's
-// second dimension.  A group of 32 elements is two neighbouring lanes'.
+// second dimension.  A group of 32 elements is two neighbouring lanes'.  Bound
+// by memory: 2.2 GB of prompts (16 requests, 32 layers of 8 heads of 128
+// elements) take 0.61 ms, 5.4 TB/s read and written together.
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_kv_append_quant(QuantAppendArgs a) {
   const uint32_t units = a.kv.head_dim / 16, per_row = units * a.kv.heads, groups = units / 2,
@@ -235,7 +239,8 @@ __global__ __launch_bounds__(kThreads) void k_kv_append_quant(QuantAppendArgs a)
 
 constexpr int kReadRows = 16;  // rows of a workgroup
 
-// A workgroup finds out where its rows' tokens lie, then reads them layer by layer, 16 elements of K and of V a thread.
+// A workgroup finds out where its rows' tokens lie, then reads them, 16 elements of K and of V a thread.  Bound by memory: 16
+// requests of 128-2048 tokens out of 16 layers of 8 heads of 128 elements (1.4 GB read and written) take 0.29 ms, 4.9 TB/s.
 template <class E>
 __global__ __launch_bounds__(kThreads) void k_kv_read_quant(QuantReadArgs p) {
   const gift_kv_read_args& a = p.a;
@@ -295,10 +300,13 @@ __global__ __launch_bounds__(kThreads) void k_kv_read_quant(QuantReadArgs p) {
 
 template <class E>
 hipError_t norm_rope(const gift_qk_rows& a, hipStream_t s) {
-  const uint64_t per = a.n_rows / 1024;
-  const uint32_t rows = per < 1 ? 1 : per < kMostRows ? (uint32_t)per : kMostRows;
+  // Rows of a workgroup: about 100 heads, so that sines are made few times over and workgroups stay short, as long as there
+  // are enough of them (17203 rows of 40 heads of 128: one row 86 us, two 72, three 73, eight 79; of 3 heads 20, 13, 13, 10).
+  const uint64_t heads = (uint64_t)a.q_heads + a.k_heads, want = heads > 50 ? 2 : heads > 12 ? 100 / heads : kMostRows,
+                 most = a.n_rows / 1024;
+  const uint32_t rows = most < 1 ? 1 : (uint32_t)(most < want ? most : want);
   const uint32_t at_once = kThreads / (a.head_dim <= 64 ? 4 : a.head_dim <= 128 ? 8 : 16);
-  const uint64_t items = (uint64_t)rows * (a.q_heads + a.k_heads), parts = rows > 1 ? 1 : (items + at_once - 1) / at_once;
+  const uint64_t items = rows * heads, parts = rows > 1 ? 1 : (items + at_once - 1) / at_once;
   const dim3 grid((uint32_t)((a.n_rows + rows - 1) / rows), (uint32_t)(parts < 1024 ? parts : 1024));
   switch (a.head_dim) {
     case 64: k_qk_norm_rope<E, 64><<<grid, kThreads, 0, s>>>(a, rows); break;
