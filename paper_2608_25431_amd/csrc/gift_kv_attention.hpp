@@ -57,9 +57,11 @@ struct Bf16 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, UPPER));
   }
 };
-// Over a quantised cache: V has 4 bits, so that weights of 8 are enough, in one operand.
+// Over a quantised cache: V has 4 bits, so that weights of 8 are enough, in one operand.  They refer to the maximum itself,
+// whose weight is then not rounded.
 struct Bf16Quant : Bf16 {
   static constexpr int kParts = 1;
+  static constexpr float kSlack = 0.f;
   __device__ static void parts(const f32x16& p, int k, vec* w) {
 #pragma unroll
     for (int i = 0; i < 8; i++) w[0][i] = (elem)p[8 * k + i];
