@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
       auto publish = [&](uint64_t* to, int t, const f32x16& o, float m, float l, int joined) {
 #pragma unroll
         for (int q = 0; q < 8; q++)
-          __hip_atomic_store(to + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2,
+          __hip_atomic_store(to + (t * 8 + q) * kWave + lane,  // a store fills whole lines
                              __builtin_bit_cast(uint64_t, f32x2{o[2 * q], o[2 * q + 1]}), __ATOMIC_RELAXED,
                              __HIP_MEMORY_SCOPE_AGENT);
         if (t == 0)
@@ -1061,7 +1061,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
                 const uint64_t* from = place(w + (j + u < n ? j + u : n - 1) * step);
                 ml[u] = published(from + (S::kAcc * 8 + (step > 1)) * kWave + lane);
 #pragma unroll
-                for (int q = 0; q < 8; q++) x[u][q] = published(from + ((t * 4 + q / 2) * kWave + lane) * 2 + q % 2);
+                for (int q = 0; q < 8; q++) x[u][q] = published(from + (t * 8 + q) * kWave + lane);
               }
               float mn = m;
 #pragma unroll

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
   auto publish = [&](uint64_t* to, int t, const f32x4& x, float m, float l, int joined) {
 #pragma unroll
     for (int h = 0; h < 2; h++)
-      __hip_atomic_store(to + (t * kWave + lane) * 2 + h, __builtin_bit_cast(uint64_t, f32x2{x[2 * h], x[2 * h + 1]}),
+      __hip_atomic_store(to + (t * 2 + h) * kWave + lane, __builtin_bit_cast(uint64_t, f32x2{x[2 * h], x[2 * h + 1]}),
                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (t == 0)
       __hip_atomic_store(to + (S::kAcc * 2 + joined) * kWave + lane, __builtin_bit_cast(uint64_t, f32x2{m, l}),
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
                 const uint64_t* from = place(w + (j + u < n ? j + u : n - 1) * step, w0);
                 ml[u] = published(from + (S::kAcc * 2 + (step > 1)) * kWave + lane);
 #pragma unroll
-                for (int h = 0; h < 2; h++) y[u][h] = published(from + (t * kWave + lane) * 2 + h);
+                for (int h = 0; h < 2; h++) y[u][h] = published(from + (t * 2 + h) * kWave + lane);
               }
               float mn = m;
 #pragma unroll
