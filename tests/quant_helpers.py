@@ -87,7 +87,7 @@ class Requests:
     """Requests with all their tokens, those of their rows last, in scattered blocks of a quantised cache."""
 
     def __init__(self, lens, rows, dtype="bf16", heads=2, group=2, dim=64, block=16, order="head", parts=1, n_layers=2,
-                 layer=1, mask=None, seed=0, spare=2, q_scale=1.0, poison=0):
+                 layer=1, mask=None, seed=0, spare=2, q_scale=1.0, kv_scale=(1.0, 1.0)):
         r = np.random.default_rng(seed)
         g = torch.Generator().manual_seed(seed)
         self.lens, self.rows, self.dtype, self.layer, self.group = np.asarray(lens), np.asarray(rows), dtype, layer, group
@@ -97,10 +97,8 @@ class Requests:
         self.tab = np.full((n, self.width), NO_BLOCK, np.int64)
         self.tab[np.arange(self.width)[None, :] < have[:, None]] = r.permutation(self.cache.n_blocks)[:have.sum()]
         total, count = int(self.lens.sum()), int(self.rows.sum())
-        x = torch.randn(2, total, heads, dim, generator=g).to(DT[dtype]).double().numpy()
-        b, f = quantised(x, dtype)
-        for _ in range(poison):  # some elements of V are no numbers
-            b[1, r.integers(total), r.integers(heads), r.integers(dim)] = NAN
+        x = torch.randn(2, total, heads, dim, generator=g) * torch.tensor(kv_scale).view(2, 1, 1, 1)
+        b, f = quantised(x.to(DT[dtype]).double().numpy(), dtype)
         self.pos = np.concatenate([np.arange(x) for x in self.lens]) if total else np.zeros(0, np.int64)
         self.req = np.repeat(np.arange(n), self.lens)
         at = (torch.from_numpy(self.tab[self.req, self.pos // block]).to(DEV), torch.from_numpy(self.pos % block).to(DEV))

@@ -5,7 +5,7 @@ import torch
 
 from kv_helpers import DEV, DT, NO_BLOCK, i32
 from paper_2608_25431_amd import gift
-from quant_helpers import NAN, Requests
+from quant_helpers import NAN, QuantCache, Requests, quantised, values
 
 pytestmark = pytest.mark.gpu
 
@@ -112,6 +112,43 @@ def test_large_scores(work):
         r.check(r.run(work))
         r.check(r.run(work, scale=-0.3), scale=-0.3)
         r.check(r.run(work, scale=0.0), scale=0.0)
+
+
+@pytest.mark.parametrize("dtype,small", [("bf16", 2.0 ** -90), ("f16", 2.0 ** -19)])
+@pytest.mark.parametrize("rows", [[1, 1], [20, 60]])
+def test_small_values(work, dtype, small, rows):
+    """K and V far below 1, in float16 below its normal numbers: neither is taken for zero."""
+    r = Requests(np.array([5, 12]) + rows, rows, dtype, 2, 2, 64, 16, kv_scale=(small, small), q_scale=1.0)
+    got = r.run(work, scale=float(0.125 / small))
+    r.check(got, scale=float(0.125 / small))
+    assert (got[0] != 0).double().mean() > 0.9
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_offsets_past_32_bits(work, rows):
+    """A cache of more than 4 GiB, of which the last blocks are in use: written, attended and read back."""
+    heads, dim, block, blocks = 8, 128, 16, 140000
+    cache = QuantCache(heads, dim, block, blocks)
+    assert cache.data.numel() > 1 << 32
+    length = 50
+    table = i32([[blocks - 1, 3, blocks - 2, blocks - 5]])
+    x = torch.randn(2, 1, length, heads, dim, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    pos = np.arange(length)
+    slots = torch.from_numpy(table.cpu().numpy()[0][pos // block].astype(np.int64) * block + pos % block).to(DEV)
+    k, v = x.to(DEV)
+    gift.kv_append_quant(*cache.args(), slots, k, v)
+    back = torch.empty_like(x, device=DEV)
+    gift.kv_read_quant(*cache.args(), table, i32([length]), i32([0, length]), back[0], back[1])
+    want = [values(*quantised(y.double().numpy(), "bf16"), "bf16") for y in x]
+    assert all((b.double().cpu().numpy() == w).all() for b, w in zip(back, want))
+    q = torch.randn(rows, heads, dim, generator=torch.Generator().manual_seed(2)).to(DEV, torch.bfloat16)
+    out = torch.empty_like(q)
+    gift.quant_attention(work, *cache.args(), 0, q, i32([0, rows]), i32([length]), table, out)
+    small = QuantCache(heads, dim, block, 4)  # the same tokens in a small cache
+    gift.kv_append_quant(*small.args(), torch.arange(length, device=DEV), k, v)
+    same = torch.empty_like(q)
+    gift.quant_attention(work, *small.args(), 0, q, i32([0, rows]), i32([length]), i32([[0, 1, 2, 3]]), same)
+    assert torch.equal(out, same) and torch.isfinite(out).all()
 
 
 def test_refused_requests_and_rows_of_none(work):
