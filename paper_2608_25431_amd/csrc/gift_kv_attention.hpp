@@ -350,11 +350,19 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
   // cut evenly 24, whole 13, over 100-500 26 and 18; 16 requests of 1-16 rows over up to 500 29 and 19; one token over 512
   // 12 and 14; where columns have up to 64 tiles, 64 over 128-2048 49 and 56.
   auto few = [&](uint64_t columns) -> bool { return columns <= n_wg && columns > 128; };
+  // workgroups beyond those that run at once have nothing to do where columns are divided
+  auto in_use = [&]() -> bool {
+    if constexpr (S::kWhole > 0) {
+      if (!whole && n_wg > p.most_wg) n_wg = p.most_wg;
+    }
+    return wg < n_wg;
+  };
   auto first_of = [&](uint32_t w) -> uint64_t {
     return n_wg == total ? w : quotient(w * total, n_wg, 1.0 / (double)n_wg);
   };
   if (a.n_reqs <= kWave) {
     if constexpr (S::kWhole > 0) whole = few(uniform(__shfl((unsigned long long)running(columns_of<S>(p, said)), kWave - 1)));
+    if (!in_use()) return false;
     const uint64_t mine = units_of<S>(p, said, whole), upto = running(mine);
     total = uniform(__shfl((unsigned long long)upto, kWave - 1));
     if (!share()) return false;
@@ -376,6 +384,7 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
       __syncthreads();
       whole = few(uniform(all));
     }
+    if (!in_use()) return false;
 #pragma unroll 4
     for (uint32_t i = 0; i < per; i++) mine += units_of<S>(p, said_of(p, tid * per + i), whole);
     uint64_t upto = running(mine);
@@ -1097,6 +1106,16 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
   }
 }
 
+// Over a quantised cache, where the tables say that no column is long: a workgroup for each column that there can be, up to
+// four times as many as run at once, which begin as others end.  37 requests of up to 576 tokens with 0-63 rows of 10 heads
+// take 22 us with as many as run at once and 18 so, 70 single tokens over 100-500 (8 KV heads) 30 and 24; 400 over 32-512, six
+// times as many, 92 and 96.
+template <class S>
+uint32_t grid_of_columns(const QuantAttnArgs& a, uint32_t grid, uint64_t cols) {
+  const uint64_t tokens = (uint64_t)a.a.table_width << a.kv.block_shift;
+  return tokens <= (uint64_t)S::kWhole * kTileKeys && cols > grid && cols <= 4ull * grid ? (uint32_t)cols : grid;
+}
+
 template <class E, class S, int MINW>
 hipError_t attend(const typename S::Args& a, const AttnWork& w, hipStream_t s) {
   // as many workgroups as run at once: MINW waves on each SIMD, four SIMDs
@@ -1108,7 +1127,13 @@ hipError_t attend(const typename S::Args& a, const AttnWork& w, hipStream_t s) {
                  cols = (uint64_t)a.kv.heads * (a.a.n_rows * a.group / (32 * S::WQ) + a.a.n_reqs),
                  rounds = tiles / S::kTiles + 1;
   if (cols < grid && cols * rounds < grid) grid = cols * rounds ? (uint32_t)(cols * rounds) : 1;
-  k_tree_attention<E, S, MINW><<<grid, S::kThreads, 0, s>>>(a, w.mem);
+  if constexpr (S::kQuant) {
+    typename S::Args b = a;
+    b.most_wg = grid;
+    k_tree_attention<E, S, MINW><<<grid_of_columns<S>(a, grid, cols), S::kThreads, 0, s>>>(b, w.mem);
+  } else {
+    k_tree_attention<E, S, MINW><<<grid, S::kThreads, 0, s>>>(a, w.mem);
+  }
   return hipGetLastError();
 }
 

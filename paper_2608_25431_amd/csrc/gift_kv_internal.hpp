@@ -47,6 +47,7 @@ struct AttnArgs {
 // The same over a quantised cache: kv is of its elements, of one byte each, and the drafted rows of `a` are NULL.
 struct QuantAttnArgs : AttnArgs {
   KvView scales;
+  uint32_t most_wg;  // workgroups that columns are divided among; there may be more where they stay whole
 };
 // The attention's workspace: counters of the columns that are joined and of
 // runs of their parts (zero between calls: the workgroup that counts a last

@@ -520,7 +520,9 @@ hipError_t attend_rows(const QuantAttnArgs& a, const AttnWork& w, hipStream_t s)
   const uint64_t tiles = ((uint64_t)a.a.table_width << a.kv.block_shift) / kTileKeys + 2,
                  cols = (uint64_t)a.kv.heads * (a.a.n_rows * a.group / S::kCols + a.a.n_reqs), rounds = tiles / S::kTiles + 1;
   if (cols < grid && cols * rounds < grid) grid = cols * rounds ? (uint32_t)(cols * rounds) : 1;
-  k_quant_rows<E, S, MINW><<<grid, S::kThreads, 0, s>>>(a, w.mem);
+  QuantAttnArgs b = a;
+  b.most_wg = grid;
+  k_quant_rows<E, S, MINW><<<grid_of_columns<S>(a, grid, cols), S::kThreads, 0, s>>>(b, w.mem);
   return hipGetLastError();
 }
 

@@ -89,6 +89,19 @@ def test_many_requests(work, dtype, dim, most, longest):
     q.check(q.run(work))
 
 
+@pytest.mark.parametrize("rows", [1, 20])
+@pytest.mark.parametrize("in_use", [0.02, 1.0])
+def test_more_columns_than_workgroups_at_once(work, rows, in_use):
+    """Tables too short for a long column, and room for more columns than workgroups run at once: all of them in use, or so
+    few that they are divided after all."""
+    r = np.random.default_rng(rows)
+    n = 420
+    rows = np.where(r.random(n) < in_use, r.integers(1, rows + 1, n), 0)
+    rows[7] = 1
+    q = Requests(r.integers(0, 200, n) + rows, rows, "bf16", 2, 1, 64, 16, seed=3)
+    q.check(q.run(work))
+
+
 @pytest.mark.parametrize("group", [1, 3, 16, 17])
 @pytest.mark.parametrize("heads", [1, 5])
 def test_query_heads_of_a_kv_head(work, group, heads):
