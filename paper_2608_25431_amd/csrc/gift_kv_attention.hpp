@@ -441,6 +441,9 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
 // take 290 us.  Without products and exponentials the loads and stores alone take
 // 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
 // two waves a SIMD that meet once a round hide a third of that.
+// Over a quantised cache 16 requests of 512 rows over 4096 tokens (32 heads, 584
+// GFLOP) take 660 us: loads and stores 300, scores 136, exponentials 113, the
+// product with V 126.
 template <class E, class S, int MINW>
 __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S::Args p, uint8_t* work) {
   typedef typename E::vec vec;
