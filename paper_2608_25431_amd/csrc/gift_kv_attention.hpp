@@ -497,7 +497,10 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
     const uint32_t column = __builtin_amdgcn_readfirstlane(at.column), it0 = __builtin_amdgcn_readfirstlane(at.round);
     const uint64_t col_first = unit - it0, col_last = col_first + cut.units(r) - 1;
     const uint32_t it1 = !cut.whole && unit_end - unit < r.rounds - it0 ? (uint32_t)(it0 + (unit_end - unit)) : r.rounds;
-    const uint32_t g = __builtin_amdgcn_readfirstlane(quotient(column, r.col_tiles)), ct = column - g * r.col_tiles;
+    const uint32_t g = __builtin_amdgcn_readfirstlane(quotient(column, r.col_tiles));
+    uint32_t ct = column - g * r.col_tiles;
+    // of a chunk the first columns and the last in turn, which see few of its tokens and many
+    if (S::kQuant && !a.mask) ct = ct & 1 ? r.col_tiles - 1 - ct / 2 : ct / 2;
     // this lane's query row
     const uint32_t rows = r.rows * p.group, qrow = (ct * S::WQ + wq) * 32 + col;
     const bool qlive = qrow < rows;
@@ -506,7 +509,16 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
     const uint64_t qtok = r.row0 + token;
     State<S> st;
     st.clear();
-    if (!r.dead && r.tiles) {
+    // Rounds behind the last key that a row of the column sees are only counted: with the order of columns above, 16 prompts of
+    // 2048 tokens (32 heads) take 840 us instead of 1160, one of 4096 201 instead of 324.
+    uint32_t stop = it1;
+    if (S::kQuant && !a.mask) {
+      const uint32_t last = ct * S::kCols + S::kCols - 1;
+      const int32_t key = (int32_t)(r.len - r.rows + quotient(last < rows ? last : rows - 1, p.group));
+      const uint32_t needed = key < 0 ? 0u : (uint32_t)key / (kTileKeys * S::kTiles) + 1;
+      stop = __builtin_amdgcn_readfirstlane(needed < it1 ? needed : it1);
+    }
+    if (!r.dead && r.tiles && (!S::kQuant || it0 < stop)) {
       // Queries: in registers, or in LDS where all waves have the same ones and need the registers for keys on their way.
       vec q[S::kQueriesInLds ? 1 : S::D / 16];
       if constexpr (!S::kQueriesInLds) {
@@ -526,7 +538,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
       // rows of the round between, since loads come back in order and the addresses wait for it.
       auto block_of = [&](uint32_t it) -> uint32_t {
         const uint32_t j = (it * S::kTiles + wk * S::TK) * kTileKeys + my_row;
-        return *(it < it1 && j < r.len ? tab + (j >> p.kv.block_shift) : a.row_begin);  // no branch around the load
+        return *(it < stop && j < r.len ? tab + (j >> p.kv.block_shift) : a.row_begin);  // no branch around the load
       };
       // Second step: this lane's row.
       struct Row {
@@ -544,10 +556,10 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
         x.drafted = x.any && (S::kQuant ? reaches_own(j) : j >= ctx_keys);
         x.k = kbase + id * p.kv.block_stride + (j & ((1u << p.kv.block_shift) - 1)) * p.kv.token_stride;
         x.v = x.k + p.kv.v_off;
-        x.ok = it < it1 && j < r.len && id < p.kv.n_blocks;
+        x.ok = it < stop && j < r.len && id < p.kv.n_blocks;
         if (!S::kQuant && x.drafted) {
           const uint32_t t = j - ctx_keys;
-          x.ok = it < it1 && a.k && t < r.rows;
+          x.ok = it < stop && a.k && t < r.rows;
           x.k = dk + t * a.k_row_stride;
           x.v = dv + t * a.v_row_stride;
         }
@@ -879,7 +891,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
         __syncthreads();
         for (uint32_t it = it0;; it++) {
           const uint32_t t = it * S::kTiles + wk;
-          const bool more = it + 1 < it1;
+          const bool more = it + 1 < stop;
           f32x16 sc[1];
           if constexpr (S::kQuant) {
             store_k(x, row, 0);
@@ -923,7 +935,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
           const uint32_t buf = (it - it0) & 1;
           store_k(xk, row, buf);
           store_v(xv, row, buf);
-          if (it + 1 < it1) {
+          if (it + 1 < stop) {
             id = next;
             next = block_of(it + 2);
             row = row_of(it + 1, id);
@@ -952,7 +964,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
               __builtin_amdgcn_s_setprio(0);
             }
           }
-          if (it + 1 == it1) break;
+          if (it + 1 == stop) break;
         }
       }
       st.l += other_half(st.l);
