@@ -499,8 +499,9 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
     const uint32_t it1 = !cut.whole && unit_end - unit < r.rounds - it0 ? (uint32_t)(it0 + (unit_end - unit)) : r.rounds;
     const uint32_t g = __builtin_amdgcn_readfirstlane(quotient(column, r.col_tiles));
     uint32_t ct = column - g * r.col_tiles;
-    // of a chunk the first columns and the last in turn, which see few of its tokens and many
-    if (S::kQuant && !a.mask) ct = ct & 1 ? r.col_tiles - 1 - ct / 2 : ct / 2;
+    // of a chunk that is most of its request the first columns and the last in turn, which see few of its tokens and many (of
+    // shorter ones it costs 4%)
+    if (S::kQuant && !a.mask && 2ull * r.rows > r.len) ct = ct & 1 ? r.col_tiles - 1 - ct / 2 : ct / 2;
     // this lane's query row
     const uint32_t rows = r.rows * p.group, qrow = (ct * S::WQ + wq) * 32 + col;
     const bool qlive = qrow < rows;
