@@ -188,6 +188,31 @@ def test_read_rows_of_no_request_stay():
     assert (got[0, 0, 2:4] == r.k[:2]).all() and (got[1, 0, 4:10] == r.v[4:]).all()
 
 
+def test_read_into_one_buffer_on_a_stream_and_replayed():
+    """K and V heads beside each other in a row, behind others that stay; eager on a stream of its own, then from a graph."""
+    r = Requests([30, 7], [0, 0], "bf16", 3, 1, 64, 8)
+    out = torch.full((1, 37, 8, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    args = (i32(r.tab), i32(r.lens), i32([0, 30, 37]), out[:, :, 2:5], out[:, :, 5:])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    gift.kv_read_quant(*r.cache.args(), *args, layer=r.layer, stream=s)
+    s.synchronize()
+
+    def check():
+        got = out[0].double().cpu().numpy()
+        assert (got[:, :2] == 7).all() and (got[:, 2:5] == r.k).all() and (got[:, 5:] == r.v).all()
+
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gift.kv_read_quant(*r.cache.args(), *args, layer=r.layer)
+    for _ in range(3):
+        out[:, :, 2:] = 0
+        graph.replay()
+        torch.cuda.synchronize()
+        check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_read_every_element_and_factor(dtype):
     """Every element with the factors that may be written; f16: rounded to the type, past its range infinite."""
@@ -210,7 +235,7 @@ def test_read_every_element_and_factor(dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_back_and_forth(dtype):
-    """What is read back is off by half a step of an element at most, and quantises to the same bytes again."""
+    """What is read back is off by half a step of an element at most, and quantises to the same values again."""
     cache = QuantCache(2, 128, 16, 4)
     x = rows_of(dtype, 2, 1, 50, 2, 128)
     append(cache, x, dtype, range(50))
@@ -222,9 +247,7 @@ def test_back_and_forth(dtype):
     # elements: 4 bits (half a step 2^-4), or steps of 2^-9 of a factor that is at most 2 / 448 of the largest
     bound = np.maximum(np.abs(x) * 2.0 ** -4, np.broadcast_to(top * 2.0 ** -10 * 2 / 448, x.shape[:-1] + (4, 32)).reshape(x.shape))
     assert (np.abs(x - y) <= np.maximum(bound, 2.0 ** -110)).all()
-    before = cache.data.clone()
     gift.kv_append_quant(*cache.args(), torch.arange(50, device=DEV), out[0], out[1])
     read_again = torch.empty_like(out)
     gift.kv_read_quant(*cache.args(), *args, read_again[0], read_again[1])
     assert torch.equal(out, read_again)
-    assert before.shape == cache.data.shape

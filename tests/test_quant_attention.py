@@ -51,6 +51,15 @@ def test_own_tokens_begin_anywhere_in_a_tile(work, start, mask):
     r.check(r.run(work))
 
 
+@pytest.mark.parametrize("lens,rows", [([700], [700]), ([650, 40, 700], [650, 40, 300]), ([1100, 90], [400, 90]),
+                                       ([300, 500], [310, 520])])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_whole_prompts(work, lens, rows, dim):
+    """Chunks of many column tiles, of which the first see little: whole prompts, parts of them, more rows than tokens."""
+    r = Requests(lens, rows, "bf16", 1, 2, dim, 16, seed=8)
+    r.check(r.run(work))
+
+
 def test_mask_of_fewer_words_than_rows(work):
     """Rows past 32 * mask_words are not seen."""
     r = Requests([150], [70], "f16", 2, 2, 64, 16, mask="random")
