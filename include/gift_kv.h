@@ -383,11 +383,9 @@ typedef struct {
  *     is set; rows past 32 * mask_words are not seen; without a mask, j <= i.
  * K and V are the values of the cache's elements in the type of q, as
  * gift_kv_read_quant gives them (factor bytes 0 and 255, which are never
- * written, give values that are not defined).  The weights are rounded to the
- * type of q once (V has 4 bits; the sum is of unrounded ones).  All else is as in
- * gift_tree_attention: rows that see nothing, verdicts, table entries outside
- * the cache, what is not seen, the other roundings, workspaces, overlaps and
- * errors.
+ * written, give values that are not defined).  All else, roundings among it, is
+ * as in gift_tree_attention: rows that see nothing, verdicts, table entries
+ * outside the cache, what is not seen, workspaces, overlaps and errors.
  */
 gift_status gift_quant_attention(gift_attention_work work, const gift_paged_kv* kv, const gift_kv_format* format,
                                  const gift_kv_scales* scales, const gift_quant_attention_args* args,

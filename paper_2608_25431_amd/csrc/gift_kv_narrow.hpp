@@ -380,9 +380,11 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
         }
 
         // V^T P^T: a lane's weights are those of keys 4 part .. 4 part + 3 and of the same behind 16
-        vec w;
+        f32x16 weights;  // of which the first half is in use
 #pragma unroll
-        for (int i = 0; i < 8; i++) w[i] = (typename E::elem)sc[i / 4][i % 4];
+        for (int i = 0; i < 8; i++) weights[i] = sc[i / 4][i % 4];
+        vec w[E::kParts];
+        E::parts(weights, 0, w);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         typedef __attribute__((address_space(3))) s16x4 lds4;
@@ -396,7 +398,8 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs 
           Frag u;
           u.x[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 32 * d));
           u.x[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(vrow + 32 * d + 16 * S::kVRow));
-          o[d] = mfma16(u.v, w, o[d]);
+#pragma unroll
+          for (int e = 0; e < E::kParts; e++) o[d] = mfma16(u.v, w[e], o[d]);
         }
         if (!more) break;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

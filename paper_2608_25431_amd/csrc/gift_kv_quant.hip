@@ -367,7 +367,7 @@ hipError_t launch_kv_read_quant(const QuantReadArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s) {
-  return dtype == GIFT_BF16 ? attend_quantised<Bf16Quant>(a, w, s) : attend_quantised<F16>(a, w, s);
+  return dtype == GIFT_BF16 ? attend_quantised<Bf16>(a, w, s) : attend_quantised<F16>(a, w, s);
 }
 
 }  // namespace gift
