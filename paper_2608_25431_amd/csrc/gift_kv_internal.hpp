@@ -64,6 +64,11 @@ struct AttnWork {
 hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
 hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
 
+// How a call is cut by rows: those of a workgroup of 256 threads, workgroups that share them, and rows of a launch.
+struct RowsPlan {
+  uint32_t rows, parts, launch;
+};
+RowsPlan qk_norm_rope_plan(const gift_qk_rows& a);
 hipError_t launch_qk_norm_rope(const gift_qk_rows& a, hipStream_t s);
 
 struct QuantAppendArgs {

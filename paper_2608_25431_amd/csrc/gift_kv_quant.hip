@@ -11,6 +11,9 @@ namespace gift {
 namespace {
 
 constexpr int kThreads = 256;
+// Workgroups of a launch.  One of 2^32 threads along a dimension or more runs nothing, without an error, so that more rows
+// take another launch.
+constexpr uint32_t kMostGroups = 1u << 18;
 
 template <class E>
 __device__ inline float upper_of(uint32_t x) {
@@ -299,15 +302,9 @@ __global__ __launch_bounds__(kThreads) void k_kv_read_quant(QuantReadArgs p) {
 }
 
 template <class E>
-hipError_t norm_rope(const gift_qk_rows& a, hipStream_t s) {
-  // Rows of a workgroup: about 100 heads, so that sines are made few times over and workgroups stay short, as long as there
-  // are enough of them (17203 rows of 40 heads of 128: one row 86 us, two 72, three 73, eight 79; of 3 heads 20, 13, 13, 10).
-  const uint64_t heads = (uint64_t)a.q_heads + a.k_heads, want = heads > 50 ? 2 : heads > 12 ? 100 / heads : kMostRows,
-                 most = a.n_rows / 1024;
-  const uint32_t rows = most < 1 ? 1 : (uint32_t)(most < want ? most : want);
-  const uint32_t at_once = kThreads / (a.head_dim <= 64 ? 4 : a.head_dim <= 128 ? 8 : 16);
-  const uint64_t items = rows * heads, parts = rows > 1 ? 1 : (items + at_once - 1) / at_once;
-  const dim3 grid((uint32_t)((a.n_rows + rows - 1) / rows), (uint32_t)(parts < 1024 ? parts : 1024));
+hipError_t norm_rope(const gift_qk_rows& a, const RowsPlan& plan, hipStream_t s) {
+  const uint32_t rows = plan.rows;
+  const dim3 grid((uint32_t)((a.n_rows + rows - 1) / rows), plan.parts);
   switch (a.head_dim) {
     case 64: k_qk_norm_rope<E, 64><<<grid, kThreads, 0, s>>>(a, rows); break;
     case 96: k_qk_norm_rope<E, 96><<<grid, kThreads, 0, s>>>(a, rows); break;
@@ -342,8 +339,32 @@ hipError_t attend_quantised(const QuantAttnArgs& a, const AttnWork& w, hipStream
 
 }  // namespace
 
+RowsPlan qk_norm_rope_plan(const gift_qk_rows& a) {
+  // Rows of a workgroup: about 100 heads, so that sines are made few times over and workgroups stay short, as long as there
+  // are enough of them (17203 rows of 40 heads of 128: one row 86 us, two 72, three 73, eight 79; of 3 heads 20, 13, 13, 10).
+  const uint64_t heads = (uint64_t)a.q_heads + a.k_heads, want = heads > 50 ? 2 : heads > 12 ? 100 / heads : kMostRows,
+                 most = a.n_rows / 1024;
+  const uint32_t rows = most < 1 ? 1 : (uint32_t)(most < want ? most : want);
+  const uint32_t at_once = kThreads / (a.head_dim <= 64 ? 4 : a.head_dim <= 128 ? 8 : 16);
+  const uint64_t items = rows * heads, parts = rows > 1 ? 1 : (items + at_once - 1) / at_once;
+  return RowsPlan{rows, (uint32_t)(parts < 1024 ? parts : 1024), kMostGroups * rows};
+}
+
 hipError_t launch_qk_norm_rope(const gift_qk_rows& a, hipStream_t s) {
-  return a.dtype == GIFT_BF16 ? norm_rope<Bf16>(a, s) : norm_rope<F16>(a, s);
+  const RowsPlan plan = qk_norm_rope_plan(a);
+  for (uint64_t row = 0; row < a.n_rows; row += plan.launch) {
+    auto from = [&](const void* p, uint64_t stride) -> void* { return p ? (uint8_t*)p + row * stride : nullptr; };
+    gift_qk_rows b = a;
+    b.n_rows = a.n_rows - row < plan.launch ? a.n_rows - row : plan.launch;
+    b.q = from(a.q, a.q_row_stride);
+    b.k = from(a.k, a.k_row_stride);
+    b.q_out = from(a.q_out, a.q_out_row_stride);
+    b.k_out = from(a.k_out, a.k_out_row_stride);
+    b.positions = (const int32_t*)from(a.positions, 4);
+    const hipError_t e = a.dtype == GIFT_BF16 ? norm_rope<Bf16>(b, plan, s) : norm_rope<F16>(b, plan, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_kv_append_quant(const QuantAppendArgs& a, uint32_t dtype, hipStream_t s) {
