@@ -64,7 +64,8 @@ struct AttnWork {
 hipError_t launch_tree_attention(const AttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
 hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s);
 
-// How a call is cut by rows: those of a workgroup of 256 threads, workgroups that share them, and rows of a launch.
+// How a call is cut by rows: those of a workgroup of 256 threads, workgroups that share them (their heads,
+// or layers), and rows of a launch.
 struct RowsPlan {
   uint32_t rows, parts, launch;
 };
@@ -83,7 +84,9 @@ hipError_t launch_kv_append_quant(const QuantAppendArgs& a, uint32_t dtype, hipS
 struct QuantReadArgs {
   KvView kv, scales;
   gift_kv_read_args a;
+  uint64_t row0;  // the first row of a launch
 };
+RowsPlan kv_read_quant_plan(const gift_kv_read_args& a);
 hipError_t launch_kv_read_quant(const QuantReadArgs& a, hipStream_t s);
 
 }  // namespace gift

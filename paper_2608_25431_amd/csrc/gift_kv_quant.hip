@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_read_quant(QuantReadArgs p) {
   const gift_kv_read_args& a = p.a;
   __shared__ int64_t slots[kReadRows];  // -1: zeros, -2: left as it is
   const uint32_t tid = threadIdx.x, units = p.kv.head_dim / 16, per_row = units * p.kv.heads;
-  const uint64_t row0 = (uint64_t)blockIdx.x * kReadRows;
+  const uint64_t row0 = p.row0 + (uint64_t)blockIdx.x * kReadRows;
   if (tid < kReadRows) {
     const uint64_t r = row0 + tid;
     int64_t slot = -2;
@@ -377,14 +377,25 @@ hipError_t launch_kv_append_quant(const QuantAppendArgs& a, uint32_t dtype, hipS
   return hipGetLastError();
 }
 
+RowsPlan kv_read_quant_plan(const gift_kv_read_args& a) {
+  return RowsPlan{(uint32_t)kReadRows, a.n_layers < 65535 ? a.n_layers : 65535, kMostGroups * kReadRows};
+}
+
 hipError_t launch_kv_read_quant(const QuantReadArgs& a, hipStream_t s) {
-  const uint32_t tiles = (uint32_t)((a.a.n_rows + kReadRows - 1) / kReadRows), layers = a.a.n_layers;
-  const dim3 grid(tiles, layers < 65535 ? layers : 65535);
-  if (a.a.dtype == GIFT_BF16)
-    k_kv_read_quant<Bf16><<<grid, kThreads, 0, s>>>(a);
-  else
-    k_kv_read_quant<F16><<<grid, kThreads, 0, s>>>(a);
-  return hipGetLastError();
+  const RowsPlan plan = kv_read_quant_plan(a.a);
+  for (uint64_t row = 0; row < a.a.n_rows; row += plan.launch) {
+    QuantReadArgs b = a;
+    b.row0 = row;
+    const uint64_t rows = a.a.n_rows - row < plan.launch ? a.a.n_rows - row : plan.launch;
+    const dim3 grid((uint32_t)((rows + plan.rows - 1) / plan.rows), plan.parts);
+    if (a.a.dtype == GIFT_BF16)
+      k_kv_read_quant<Bf16><<<grid, kThreads, 0, s>>>(b);
+    else
+      k_kv_read_quant<F16><<<grid, kThreads, 0, s>>>(b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_quant_attention(const QuantAttnArgs& a, uint32_t dtype, const AttnWork& w, hipStream_t s) {
