@@ -338,7 +338,8 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
     }
     return v;
   };
-  // Columns that are not long stay whole where no workgroup has more than one and there are enough of them: what joining
+  // Columns that are not long stay whole where no workgroup has more than one and there are enough of them, more than for half
+  // of the 256 CUs (single tokens over 100-600, 128 columns: cut evenly 11.8 us, whole 13.1; 160: 18.8 and 13.3): what joining
   // costs is then more than what an even cut gives.  In us, over a quantised cache: 64 single tokens over 32-256 cached ones
   // cut evenly 24, whole 13, over 100-500 26 and 18; 16 requests of 1-16 rows over up to 500 29 and 19; one token over 512
   // 12 and 14; where columns have up to 64 tiles, 64 over 128-2048 49 and 56.
@@ -435,8 +436,9 @@ __device__ __forceinline__ bool cut_work(const Args& p, uint32_t tid, uint32_t w
 // 183 us of it; scores add about 70, exponentials 50, the product with V 100, and
 // two waves a SIMD that meet once a round hide a third of that.
 // Over a quantised cache 16 requests of 512 rows over 4096 tokens (32 heads, 584
-// GFLOP) take 660 us: loads and stores 300, scores 136, exponentials 113, the
-// product with V 126.
+// GFLOP) take 810 us in bfloat16, whose weights are two operands, and 665 in
+// float16: without scores 614 and 483, without exponentials 704 and 532, without
+// the product with V 458 and 511, without all of these 216.
 template <class E, class S, int MINW>
 __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S::Args p, uint8_t* work) {
   typedef typename E::vec vec;
@@ -504,7 +506,7 @@ __global__ __launch_bounds__(S::kThreads, MINW) void k_tree_attention(typename S
     State<S> st;
     st.clear();
     // Rounds behind the last key that a row of the column sees are only counted: with the order of columns above, 16 prompts of
-    // 2048 tokens (32 heads) take 840 us instead of 1160, one of 4096 201 instead of 324.
+    // 2048 tokens (32 heads, bfloat16) take 940 us instead of 1590, one of 4096 214 instead of 388.
     uint32_t stop = it1;
     if (S::kQuant && !a.mask) {
       const uint32_t last = ct * S::kCols + S::kCols - 1;

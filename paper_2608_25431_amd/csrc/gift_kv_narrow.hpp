@@ -30,6 +30,8 @@ template <int D_, int W_>
 struct Narrow {
   typedef QuantAttnArgs Args;
   static constexpr int D = D_, kCols = 16, kWaves = W_, kThreads = kWave * kWaves, kTiles = kWaves, kPieces = D / 8;
+  // in token order, back to back: 64 single tokens over 128-2048 take 56 us with neighbours on one XCD and 50 without, one
+  // over 131072 74 and 73
   static constexpr bool kNeighbours = false;
   static constexpr uint32_t kWhole = 20;
   static constexpr int kSteps = D / 32;                       // of 32 elements of a score's product
@@ -46,11 +48,14 @@ struct Narrow {
 // quarter of the elements of two keys, whose addresses it works out itself: keys go from memory to the products in
 // registers, since the order of elements in a product is free (the queries are read in the same order), and only V
 // goes through LDS, to be transposed.
-// Bound by memory: K and V of 131072 tokens (8 heads of 128 elements, 277 MB) take 70 us where a head's tokens follow each
-// other and 82 where heads lie between them, 4.0 and 3.4 TB/s: 5.2 while keys are read (from 65536 tokens to 262144), and
-// about 17 us for the launch, the first loads and the joining of parts.  Products and exponentials show as 2 us of it.
-// Three workgroups a CU take longer (104 us), and so do loads that pass the caches (92), the next column's first loads ahead
-// of this one's joining (64 single tokens over 128-2048: 51 to 54 us instead of 49) and cuts moved to columns' ends (51).
+// Bound by memory: K and V of 131072 tokens (8 heads of 128 elements, 277 MB) take 62 us where a head's tokens follow each
+// other and 73 where heads lie between them, call after call: 4.5 and 3.8 TB/s, 5.6 and 4.7 while keys are read (from 65536
+// tokens to 131072), and about 13 us for the launch, the first loads and the joining of parts.  Of 64 single tokens over
+// 128-2048 in token order (50 us) 194 MB come from memory where 155 are needed: 32 bytes hold a token's factors of all heads,
+// and heads run on different XCDs, each of which fetches the line (head by head 164 MB and 47 us).
+// In a kernel trace, where 131072 tokens with heads between take 82 us and 64 single ones 49: three workgroups a CU 104, loads
+// that pass the caches 92; the next column's first loads ahead of this one's joining 51 to 54, cuts moved to columns' ends 51,
+// no products and exponentials 47.
 template <class E, class S, int MINW>
 __global__ __launch_bounds__(S::kThreads, MINW) void k_quant_rows(QuantAttnArgs p, uint8_t* work) {
   typedef typename E::vec vec;
